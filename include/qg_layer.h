@@ -1,0 +1,120 @@
+/*
+ * qg_layer.h -- C ABI of what stands between the matrix products of a decoder layer
+ *
+ * The products are qgemm.h's.  A layer that serves low-bit weights with int8 activations and an 8-bit
+ * attention cache needs, around them:
+ *
+ *   qg_rmsnorm_a8    residual addition, root-mean-square norm, int8 rows for qgemm_a8
+ *   qg_silu_a8       the gated activation, int8 rows for qgemm_a8
+ *   qg_kv_append     rotary positions on queries and keys, keys and values into a paged 8-bit cache
+ *   qg_kv_attention  attention over that cache, for single tokens and for prompts
+ *   qg_kv_dequant    the cache's values written out in 16 bits, to be looked at
+ *
+ * Conventions are those of qgemm.h: device pointers owned by the caller, work enqueued on `stream`, a qg_status
+ * returned (negative: nothing was enqueued), hipStreamPerThread refused where a workspace may be needed.
+ * Different from there: rows may have a stride (in elements, between the starts of consecutive rows), and 16-bit
+ * inputs may lie at any multiple of 2 bytes; where pointers and strides are multiples of 16 bytes and the width
+ * is one of 8 elements, rows are read 16 bytes at a time.
+ *
+ * The 8-bit rule, everywhere: QMAX = 127 for int8, 448 for e4m3;
+ *        scale = max(amax / QMAX, 2^-40)     amax: largest magnitude of the row, or of the block's values
+ *        code  = rne(x * (1 / scale)), clamped to +-QMAX            value = code * scale
+ * All of it in fp32.  Where amax is infinite or NaN the scale is NaN, so what is computed from it is NaN too.
+ * The floor keeps 1 / scale finite and a block of zeros comparable with its neighbours.
+ */
+#ifndef QG_LAYER_H_
+#define QG_LAYER_H_
+
+#include "qgemm.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* h = x + residual;  y = h / sqrt(mean(h^2) + eps) * weight;  A8, a_scale = 8-bit rows of y (int8).
+ *   x, residual  [M, N] of `act` (QG_F16 / QG_BF16), row strides x_stride, residual_stride >= N; residual may be NULL
+ *   weight       [N] of `act`
+ *   sum_out      [M, N] of `act`, row stride sum_stride: h rounded to nearest even.  May be NULL, may be `residual` or
+ *                `x` itself (with its stride); otherwise outputs must not overlap inputs
+ *   A8           [M, N] int8, contiguous, 8-byte aligned where N is a multiple of 8;   a_scale  [M] fp32
+ * h, the sum and the norm are fp32 (h is not rounded before the norm).  M >= 0, 1 <= N <= 2^24, eps >= 0.
+ * QG_EINVAL on null or misaligned pointers, strides below N, a negative or NaN eps. */
+QG_API int qg_rmsnorm_a8(const void* x, const void* residual, const void* weight, float eps, int act, int64_t M, int64_t N,
+                  int64_t x_stride, int64_t residual_stride, int8_t* A8, float* a_scale, void* sum_out, int64_t sum_stride,
+                  void* stream);
+
+/* y = gate / (1 + exp(-gate)) * up;  A8, a_scale = 8-bit rows of y (int8).
+ *   gate, up     [M, N] of `act`, row strides gate_stride, up_stride >= N: as a fused projection leaves them, up = gate + N
+ *                and both strides 2 N
+ *   A8, a_scale  as for qg_rmsnorm_a8 */
+QG_API int qg_silu_a8(const void* gate, const void* up, int act, int64_t M, int64_t N, int64_t gate_stride, int64_t up_stride,
+               int8_t* A8, float* a_scale, void* stream);
+
+/* The paged cache.  A block holds QG_KV_BLOCK tokens of every key/value head; per block and head there are one scale for
+ * the keys and one for the values.
+ *   k_cache, v_cache   [num_blocks, kv_heads, 64 * head_dim] bytes, 16-byte aligned
+ *   k_scale, v_scale   [num_blocks, kv_heads] fp32
+ *   type               {QG_INT, 8, 0, 0} (stored offset-binary, as integer weights are) or {QG_FLOAT, 8, 4, 3}
+ * Inside a (block, head) bytes lie in the order in which the lanes of a wavefront load them as operands of the 16x16x32
+ * matrix instruction, so that neither kernel moves them between lanes:
+ *   keys    token 16 t + i, dimension 64 c + 16 b + e   at   (((t * head_dim/64 + c) * 4 + b) * 16 + i) * 16 + e
+ *   values  token 16 t + 4 b + r, dimension 16 f + i    at   ((f * 4 + b) * 16 + i) * 16 + 4 t + r
+ * head_dim is 64 or 128 (others: QG_EUNSUPPORTED).
+ *
+ * Sequences.  New rows of all sequences lie one after the other:
+ *   row_start    [batch + 1] int32: rows row_start[b] .. row_start[b+1] - 1 are sequence b's (none is fine)
+ *   kv_len       [batch] int32: tokens of sequence b in the cache with its new rows, which are the last ones: row j of n
+ *                is token kv_len[b] - n + j
+ *   block_table  [batch, table_width] int32: block of tokens 64 i .. 64 i + 63 of sequence b at [b, i].  An entry outside
+ *                0 .. num_blocks - 1 stands for no block: nothing is appended to it, none of its tokens is seen
+ *   rows         rows in all (row_start[batch] at most; what lies beyond is not touched)
+ *   max_rows     at least the most rows of one sequence: rows beyond it are not served.  Host knowledge that
+ *                sizes the grid
+ * No two sequences may append to one block; blocks that are only read may be shared. */
+#define QG_KV_BLOCK 64
+
+/* Keys and values of new rows into the cache, queries into q_out, rotated on the way.
+ *   q        [rows, q_heads, head_dim] of `act` or NULL; k, v  [rows, kv_heads, head_dim]; heads contiguous, row strides
+ *            q_stride, k_stride, v_stride
+ *   q_out    [rows, q_heads, head_dim] of `act`, contiguous (may be NULL with q NULL; may be q itself if that is contiguous)
+ *   cos, sin [positions, rot_dim / 2] fp32, or both NULL: no rotation.  Row = the token's place (the last row for places beyond),
+ *            so any base, stretching or scaling for long contexts is the table's
+ *   rot_dim  leading dimensions of a head that are rotated (even, at most head_dim); neighbours 0: dimension d pairs with
+ *            d + rot_dim / 2, 1: 2 d with 2 d + 1.   y1 = x1 cos - x2 sin, y2 = x2 cos + x1 sin in fp32; q is rounded
+ *            once to `act`, keys go to 8 bits unrounded
+ * A block's scale is that of its largest value so far: the tokens that are there keep theirs while the new ones fit,
+ * and are re-coded (rne(code * old / new)) where a larger value comes, at most half a step of the new scale each time.
+ * A token that is the first of its block starts it afresh. */
+QG_API int qg_kv_append(const void* q, const void* k, const void* v, int act, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                 const float* cos, const float* sin, int64_t positions, int rot_dim, int neighbours,
+                 const int32_t* row_start, const int32_t* kv_len, const int32_t* block_table, int64_t table_width,
+                 int64_t batch, int64_t rows, int64_t max_rows, int q_heads, int kv_heads, int head_dim, qg_wtype type,
+                 int64_t num_blocks, void* k_cache, void* v_cache, float* k_scale, float* v_scale, void* q_out, void* stream);
+
+/* out[row, head] = sum_t softmax_t(scale * q[row, head] . key_t) value_t over the tokens t that the row sees: those below
+ * kv_len whose block is there, with `causal` up to the row's own, with window > 0 the last `window` of those.  A row that
+ * sees none is 0.  Head h of q reads key/value head h / (q_heads / kv_heads).
+ *   q     [rows, q_heads, head_dim] of `act`, row stride q_stride;   out  the same, contiguous
+ *   scale > 0;   max_kv at least the longest kv_len (0: table_width * 64): decides how a long cache is cut
+ * Scores, softmax statistics and sums are fp32; products run on the fp16 matrix instruction for either `act`: 8-bit codes
+ * are exact in it, bf16 queries are brought into its range by a power of two per row, probabilities (times the block's value
+ * scale, over the row's largest such) are rounded to it.
+ * Few rows per sequence (up to 64 with their heads) stream the cache once, cut along the tokens where sequences and heads alone would not fill
+ * the GPU; the parts meet in the workspace that qgemm uses, in a fixed order.  Where no workspace is to be had (see qgemm.h)
+ * the call runs uncut. */
+QG_API int qg_kv_attention(const void* q, int act, int64_t q_stride, const void* k_cache, const void* v_cache, const float* k_scale,
+                    const float* v_scale, qg_wtype type, int64_t num_blocks, const int32_t* row_start, const int32_t* kv_len,
+                    const int32_t* block_table, int64_t table_width, int64_t batch, int64_t rows, int64_t max_rows, int64_t max_kv,
+                    int q_heads, int kv_heads, int head_dim, float scale, int causal, int64_t window, void* out, void* stream);
+
+/* The values of the last rows of each sequence (row_start, kv_len, rows as above, here for the rows to read):
+ * k_out, v_out [rows, kv_heads, head_dim] of `act`, value = code * scale, rounded once.  Rows without a block are 0. */
+QG_API int qg_kv_dequant(const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale, qg_wtype type,
+                  int64_t num_blocks, const int32_t* row_start, const int32_t* kv_len, const int32_t* block_table,
+                  int64_t table_width, int64_t batch, int64_t rows, int64_t max_rows, int kv_heads, int head_dim, int act,
+                  void* k_out, void* v_out, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* QG_LAYER_H_ */

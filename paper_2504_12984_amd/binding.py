@@ -28,7 +28,7 @@ TILE_K, TILE_N = 128, 64
 EXPORTS = ("qg_status_string", "qg_last_error", "qg_canonical_bytes", "qgemm_packed_bytes",
            "qg_pack_codes", "repack", "qdequant", "qgemm", "qgemm_noalloc", "qgemm_a8", "qdequant_codebook", "qgemm_codebook",
            "qg_set_knob", "qg_plan", "qg_probe_stream_read",
-           "qg_probe_mfma")
+           "qg_probe_mfma", "qg_rmsnorm_a8", "qg_silu_a8", "qg_kv_append", "qg_kv_attention", "qg_kv_dequant")
 
 
 class QgWType(ctypes.Structure):
@@ -94,6 +94,19 @@ def _load() -> ctypes.CDLL:
     lib.qg_probe_stream_read.restype = i32
     lib.qg_probe_stream_read.argtypes = [vp, sz, vp, vp]
     lib.qg_probe_mfma.restype = i32
+    f32 = ctypes.c_float
+    lib.qg_rmsnorm_a8.restype = i32
+    lib.qg_rmsnorm_a8.argtypes = [vp, vp, vp, f32, i32, i64, i64, i64, i64, vp, vp, vp, i64, vp]
+    lib.qg_silu_a8.restype = i32
+    lib.qg_silu_a8.argtypes = [vp, vp, i32, i64, i64, i64, i64, vp, vp, vp]
+    lib.qg_kv_append.restype = i32
+    lib.qg_kv_append.argtypes = [vp, vp, vp, i32, i64, i64, i64, vp, vp, i64, i32, i32, vp, vp, vp, i64, i64, i64, i64, i32, i32,
+                                 i32, QgWType, i64, vp, vp, vp, vp, vp, vp]
+    lib.qg_kv_attention.restype = i32
+    lib.qg_kv_attention.argtypes = [vp, i32, i64, vp, vp, vp, vp, QgWType, i64, vp, vp, vp, i64, i64, i64, i64, i64, i32, i32, i32,
+                                    f32, i32, i64, vp, vp]
+    lib.qg_kv_dequant.restype = i32
+    lib.qg_kv_dequant.argtypes = [vp, vp, vp, vp, QgWType, i64, vp, vp, vp, i64, i64, i64, i64, i32, i32, i32, vp, vp, vp]
     lib.qg_probe_mfma.argtypes = [i32, i32, i32, i32, vp, ctypes.POINTER(ctypes.c_double), vp]
     return lib
 
@@ -356,6 +369,184 @@ class BoundQgemmCodebook:
         if rc != QG_OK:
             raise QgError("qgemm_codebook", rc)
         return self.out
+
+
+# ---- between the products of a layer (include/qg_layer.h) ------------------------------------------
+
+KV_BLOCK = 64
+
+
+def _rows(t, name, dtype=None):
+    """A CUDA tensor whose rows are contiguous and lie at a stride that only grows: (pointer, row stride)."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda) or t.dtype not in _DT or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name} must be an fp16 or bf16 CUDA tensor of the call's type")
+    if t.stride(-1) != 1 or (t.dim() == 3 and t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError(f"{name} must have contiguous rows")
+    width = t.shape[-1] if t.dim() == 2 else t.shape[1] * t.shape[2]
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), width)
+
+
+def qg_rmsnorm_a8(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: torch.Tensor | None = None,
+                  sum_out: torch.Tensor | None = None):
+    """int8 rows of the norm of h = x + residual for qgemm_a8: (A8 int8 [M,N], a_scale fp32 [M], h).  h is x's type, in
+    `sum_out` if that is given (`residual` itself is fine); without a residual it is x and nothing is written."""
+    if x.dim() != 2:
+        raise ValueError("x must be [M,N] fp16 or bf16")
+    M, N = x.shape
+    x_ptr, x_stride = _rows(x, "x")
+    if weight.dtype != x.dtype or tuple(weight.shape) != (N,):
+        raise ValueError("weight must be [N] of x's type")
+    r_ptr, r_stride, s_ptr, s_stride = None, 0, None, 0
+    if residual is not None:
+        if tuple(residual.shape) != (M, N):
+            raise ValueError("residual must be [M,N] of x's type")
+        r_ptr, r_stride = _rows(residual, "residual", x.dtype)
+        if sum_out is None:
+            sum_out = torch.empty((M, N), dtype=x.dtype, device=x.device)
+    if sum_out is not None:
+        if tuple(sum_out.shape) != (M, N):
+            raise ValueError("sum_out must be [M,N] of x's type")
+        s_ptr, s_stride = _rows(sum_out, "sum_out", x.dtype)
+    A8 = torch.empty((M, N), dtype=torch.int8, device=x.device)
+    a_scale = torch.empty(M, dtype=torch.float32, device=x.device)
+    _check("qg_rmsnorm_a8", _lib.qg_rmsnorm_a8(x_ptr, r_ptr, _ptr(weight, "weight"), eps, _DT[x.dtype], M, N, x_stride, r_stride,
+                                               A8.data_ptr(), a_scale.data_ptr(), s_ptr, s_stride, _stream()))
+    return A8, a_scale, x if sum_out is None else sum_out
+
+
+def qg_silu_a8(gate: torch.Tensor, up: torch.Tensor | None = None):
+    """int8 rows of silu(gate) * up for qgemm_a8: (A8 int8 [M,N], a_scale fp32 [M]).  With one argument [M, 2N] its first
+    half is the gate."""
+    if gate.dim() != 2 or (up is None and gate.shape[1] % 2):
+        raise ValueError("gate must be [M,N], or [M,2N] with the up half behind it")
+    if up is None:
+        N = gate.shape[1] // 2
+        g_ptr, g_stride = _rows(gate, "gate")
+        u_ptr, u_stride = g_ptr + 2 * N, g_stride
+    else:
+        N = gate.shape[1]
+        if up.shape != gate.shape:
+            raise ValueError("up must be [M,N] of gate's type")
+        g_ptr, g_stride = _rows(gate, "gate")
+        u_ptr, u_stride = _rows(up, "up", gate.dtype)
+    M = gate.shape[0]
+    A8 = torch.empty((M, N), dtype=torch.int8, device=gate.device)
+    a_scale = torch.empty(M, dtype=torch.float32, device=gate.device)
+    _check("qg_silu_a8", _lib.qg_silu_a8(g_ptr, u_ptr, _DT[gate.dtype], M, N, g_stride, u_stride, A8.data_ptr(), a_scale.data_ptr(),
+                                         _stream()))
+    return A8, a_scale
+
+
+class KvCache:
+    """The paged 8-bit cache of one layer: blocks of 64 tokens, one scale per block and head for keys and for values.
+
+    k, v              uint8 [blocks, kv_heads, 64 * head_dim] in the order that include/qg_layer.h gives
+    k_scale, v_scale  fp32 [blocks, kv_heads]
+    t                 WType(QG_INT, 8) or WType(QG_FLOAT, 8, 4, 3)
+    """
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, t: WType, head_dim: int):
+        if k.dim() != 3 or k.dtype != torch.uint8 or k.shape[2] != KV_BLOCK * head_dim or k.shape != v.shape or v.dtype != torch.uint8:
+            raise ValueError("k and v must be uint8 [blocks, kv_heads, 64 * head_dim]")
+        for s in (k_scale, v_scale):
+            if s.dtype != torch.float32 or s.shape != k.shape[:2]:
+                raise ValueError("k_scale and v_scale must be fp32 [blocks, kv_heads]")
+        self.k, self.v, self.k_scale, self.v_scale, self.t, self.head_dim = k, v, k_scale, v_scale, t, head_dim
+        self.blocks, self.kv_heads = k.shape[:2]
+        self.type = t.c()
+        self.ptrs = (_ptr(k, "k"), _ptr(v, "v"), _ptr(k_scale, "k_scale"), _ptr(v_scale, "v_scale"))
+
+    @classmethod
+    def empty(cls, blocks: int, kv_heads: int, head_dim: int, t: WType, device="cuda"):
+        """A cache of `blocks` blocks; what is in them is undefined until it is appended to."""
+        def codes():
+            return torch.empty((blocks, kv_heads, KV_BLOCK * head_dim), dtype=torch.uint8, device=device)
+
+        def scales():
+            return torch.empty((blocks, kv_heads), dtype=torch.float32, device=device)
+        return cls(codes(), codes(), scales(), scales(), t, head_dim)
+
+
+def _sequences(row_start, kv_len, block_table):
+    """(pointers of the three, table width, batch)"""
+    batch = kv_len.shape[0]
+    if not (row_start.dtype == kv_len.dtype == block_table.dtype == torch.int32):
+        raise ValueError("row_start, kv_len and block_table must be int32")
+    if row_start.shape != (batch + 1,) or block_table.dim() != 2 or block_table.shape[0] != batch:
+        raise ValueError("row_start must be [batch + 1], kv_len [batch], block_table [batch, width]")
+    return _ptr(row_start, "row_start"), _ptr(kv_len, "kv_len"), _ptr(block_table, "block_table"), block_table.shape[1], batch
+
+
+def _heads(t, name, rows, heads, dim, dtype):
+    if t.dim() != 3 or tuple(t.shape) != (rows, heads, dim):
+        raise ValueError(f"{name} must be [rows, heads, head_dim] with the cache's head_dim")
+    return _rows(t, name, dtype)
+
+
+def qg_kv_append(k: torch.Tensor, v: torch.Tensor, cache: KvCache, row_start: torch.Tensor, kv_len: torch.Tensor,
+                 block_table: torch.Tensor, max_rows: int, q: torch.Tensor | None = None, cos: torch.Tensor | None = None,
+                 sin: torch.Tensor | None = None, neighbours: bool = False, q_out: torch.Tensor | None = None):
+    """Appends k, v [rows, kv_heads, head_dim] (views into a fused projection are fine) to the cache, rotated by cos, sin fp32
+    [positions, rot_dim / 2] if these are given; returns q rotated likewise [rows, q_heads, head_dim], or None without q.
+    row_start int32 [batch + 1], kv_len int32 [batch] (new rows included), block_table int32 [batch, width]; max_rows: at
+    least the most new rows of one sequence."""
+    rows, D = k.shape[0], cache.head_dim
+    if k.dtype not in _DT:
+        raise ValueError("k must be fp16 or bf16")
+    k_ptr, k_stride = _heads(k, "k", rows, cache.kv_heads, D, k.dtype)
+    v_ptr, v_stride = _heads(v, "v", rows, cache.kv_heads, D, k.dtype)
+    q_ptr, q_stride, q_heads = None, 0, 0
+    if q is not None:
+        q_heads = q.shape[1] if q.dim() == 3 else 0
+        q_ptr, q_stride = _heads(q, "q", rows, q_heads, D, k.dtype)
+        if q_out is None:
+            q_out = torch.empty((rows, q_heads, D), dtype=k.dtype, device=k.device)
+        elif q_out.shape != q.shape or q_out.dtype != q.dtype:
+            raise ValueError("q_out must be q's shape and type")
+    positions, rot = 0, 0
+    if cos is not None or sin is not None:
+        if cos is None or sin is None or cos.dtype != torch.float32 or sin.dtype != torch.float32 or cos.dim() != 2 or cos.shape != sin.shape:
+            raise ValueError("cos and sin must both be fp32 [positions, rot_dim / 2]")
+        positions, rot = cos.shape[0], 2 * cos.shape[1]
+    s_ptr, l_ptr, t_ptr, width, batch = _sequences(row_start, kv_len, block_table)
+    _check("qg_kv_append", _lib.qg_kv_append(
+        q_ptr, k_ptr, v_ptr, _DT[k.dtype], q_stride, k_stride, v_stride, _ptr(cos, "cos"), _ptr(sin, "sin"), positions, rot,
+        int(neighbours), s_ptr, l_ptr, t_ptr, width, batch, rows, max_rows, q_heads, cache.kv_heads, D, cache.type, cache.blocks,
+        *cache.ptrs, None if q is None else _ptr(q_out, "q_out"), _stream()))
+    return None if q is None else q_out
+
+
+def qg_kv_attention(q: torch.Tensor, cache: KvCache, row_start: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor,
+                    scale: float, max_rows: int, max_kv: int = 0, causal: bool = True, window: int = 0,
+                    out: torch.Tensor | None = None) -> torch.Tensor:
+    """Attention of q [rows, q_heads, head_dim] over the cache (arguments as for qg_kv_append; the rows are the last tokens of
+    their sequences).  max_kv: at least the longest kv_len (0: as long as the table is wide)."""
+    D = cache.head_dim
+    if q.dim() != 3:
+        raise ValueError("q must be [rows, heads, head_dim]")
+    rows, q_heads = q.shape[:2]
+    q_ptr, q_stride = _heads(q, "q", rows, q_heads, D, None)
+    if out is None:
+        out = torch.empty((rows, q_heads, D), dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out must be q's shape and type")
+    s_ptr, l_ptr, t_ptr, width, batch = _sequences(row_start, kv_len, block_table)
+    _check("qg_kv_attention", _lib.qg_kv_attention(
+        q_ptr, _DT[q.dtype], q_stride, *cache.ptrs, cache.type, cache.blocks, s_ptr, l_ptr, t_ptr, width, batch, rows, max_rows,
+        max_kv, q_heads, cache.kv_heads, D, scale, int(causal), window, _ptr(out, "out"), _stream()))
+    return out
+
+
+def qg_kv_dequant(cache: KvCache, row_start: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, rows: int,
+                  dtype: torch.dtype, max_rows: int | None = None):
+    """The cache's values of the last row_start[b+1] - row_start[b] tokens of each sequence: k, v [rows, kv_heads, head_dim]."""
+    shape = (rows, cache.kv_heads, cache.head_dim)
+    k, v = (torch.empty(shape, dtype=dtype, device=cache.k.device) for _ in range(2))
+    s_ptr, l_ptr, t_ptr, width, batch = _sequences(row_start, kv_len, block_table)
+    _check("qg_kv_dequant", _lib.qg_kv_dequant(
+        *cache.ptrs, cache.type, cache.blocks, s_ptr, l_ptr, t_ptr, width, batch, rows, rows if max_rows is None else max_rows,
+        cache.kv_heads, cache.head_dim, _DT[dtype], _ptr(k, "k"), _ptr(v, "v"), _stream()))
+    return k, v
 
 
 def qg_probe_stream_read(buf: torch.Tensor, sink: torch.Tensor):

@@ -28,6 +28,9 @@ QG_FOR_ALL_WT(QG_DECL)
 int large_launch_wt14(const GemmParams&, int, int, hipStream_t);
 int launch_reduce_tiles(const GemmParams&, int, int, hipStream_t);
 int launch_clear(void*, size_t, hipStream_t);
+size_t layer_workspace_bytes();
+int layer_workspace(size_t, size_t, hipStream_t, float**, unsigned**);
+void layer_error(const char*);
 // codebook indices of 1..8 bits: kernel-side weight types WT_LUT0 .. WT_LUT0 + 7
 #define QG_FOR_ALL_LUT(X) X(15) X(16) X(17) X(18) X(19) X(20) X(21) X(22)
 #define QG_DECL(i)                                                            \
@@ -208,6 +211,19 @@ enum WsMode { WS_PER_STREAM = 0, WS_STATIC = 1 };
 static int acquire_ws(int mode, size_t partial_bytes, size_t ticket_count, hipStream_t st, GemmParams& p) {
   return mode == WS_STATIC ? get_static_scratch(partial_bytes, ticket_count, &p.ws, &p.tickets, &p.slots)
                            : get_workspace(partial_bytes, ticket_count, st, &p.ws, &p.tickets, &p.slots);
+}
+
+// The same workspace for the kernels between a layer's products (no call of theirs throws).
+size_t layer_workspace_bytes() { return WS_PARTIAL_BYTES; }
+int layer_workspace(size_t partial_bytes, size_t counters, hipStream_t st, float** partial, unsigned** tickets) {
+  try {
+    return get_workspace(partial_bytes, counters, st, partial, tickets);
+  } catch (...) {
+    return QG_EHIP;
+  }
+}
+void layer_error(const char* text) {
+  try { g_last_error = text; } catch (...) {}
 }
 
 // Slots for a streaming kernel's exchange, in a workspace acquired for the partial sums of all its slabs.  More

@@ -1,0 +1,356 @@
+// Keys and values into the paged 8-bit cache, rotated on the way; and the cache's values written out again.
+//
+// Bound: HBM and launch (a row is read once as 16 bits, written once as 8).  The unit of work is a (sequence, block of 64
+// tokens, head, keys or values): one workgroup sees all values that share a scale, so the scale is a maximum inside it, and
+// one that grows can re-code the tokens that are there, with no second kernel and no atomics.  How many blocks the
+// sequences touch is device data: the grid has as many units as there can be, and a workgroup finds its own by adding up
+// the sequences before it, 64 at a time.
+#include "qg_layer.h"
+
+namespace qg {
+
+constexpr int KV_THREADS = 256;
+
+// Blocks that `rows` rows at the end of `length` tokens touch (rows before token 0 or past the table are nowhere).
+struct Touched { int first, count, from, upto; };       // blocks first .. first + count - 1, tokens from .. upto - 1
+__device__ __forceinline__ Touched touched(const KvParams& p, const Sequence& s) {
+  Touched t;
+  const int64_t room = p.width * KV_BLOCK;
+  t.from = max(s.before, 0);
+  t.upto = (int)min((int64_t)s.before + max(s.rows, 0), min((int64_t)s.length, room));
+  t.first = t.from / KV_BLOCK;
+  t.count = t.upto > t.from ? (t.upto - 1) / KV_BLOCK - t.first + 1 : 0;
+  return t;
+}
+
+// The unit'th touched block: its sequence (-1: there are not so many) and its place among the sequence's.
+__device__ __forceinline__ int find_unit(const KvParams& p, int unit, int l, int* nth) {
+  if (p.max_rows == 1) { *nth = 0; return unit < p.batch ? unit : -1; }        // one block each (or none)
+  int before = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += 64) {
+    int n = 0;
+    if (b0 + l < p.batch) n = touched(p, sequence(p, b0 + l)).count;
+    int sum = n;                                                               // of the lanes up to this one
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int x = __shfl_up(sum, d);
+      if (l >= d) sum += x;
+    }
+    const uint64_t over = __ballot(before + sum > unit);
+    if (over) {
+      const int at = __builtin_ctzll(over);
+      *nth = unit - before - (__shfl(sum, at) - __shfl(n, at));
+      return b0 + at;
+    }
+    before += __shfl(sum, 63);
+  }
+  return -1;
+}
+// At most so many blocks are touched.
+static int64_t most_units(const KvParams& p) {
+  const int64_t each = (int64_t)p.batch * ((p.max_rows + KV_BLOCK - 2) / KV_BLOCK + 1);
+  return std::min(each, (int64_t)p.rows / KV_BLOCK + 2 * (int64_t)p.batch);
+}
+
+// Sequence of a row: how many sequences end at or before it.
+__device__ __forceinline__ int find_sequence(const KvParams& p, int row, int l) {
+  for (int b0 = 0; b0 < p.batch; b0 += 64) {
+    const uint64_t after = __ballot(b0 + l < p.batch && p.row_start[b0 + l + 1] > row);
+    if (after) return b0 + __builtin_ctzll(after);
+  }
+  return -1;
+}
+
+// One element of a row, rotated.
+template <bool BF16>
+__device__ __forceinline__ float rotated(const KvParams& p, const uint16_t* head, int d, int64_t pos) {
+  const float x = act_to_f32<BF16>(head[d]);
+  if (d >= p.rot) return x;
+  const int half = p.rot / 2;
+  const bool second = p.neighbours ? (d & 1) : d >= half;
+  const int pair = p.neighbours ? d / 2 : (second ? d - half : d);
+  const float other = act_to_f32<BF16>(head[p.neighbours ? d ^ 1 : (second ? d - half : d + half)]);
+  const float c = p.cos[pos * half + pair], s = p.sin[pos * half + pair];
+  // products rounded on their own, so that either member of a pair is computed alike
+  return second ? __fadd_rn(__fmul_rn(x, c), __fmul_rn(other, s)) : __fsub_rn(__fmul_rn(x, c), __fmul_rn(other, s));
+}
+
+// Sixteen elements from dimension d0 on (a multiple of 16).  Wide rows: 16-byte loads, and a rotation whose partners of 16
+// neighbouring elements are 16 neighbouring ones too (or the same).
+template <bool BF16, bool ROTATE>
+__device__ __forceinline__ void sixteen(const KvParams& p, const uint16_t* head, int d0, int64_t pos, float (&x)[16]) {
+  if (!p.wide) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = ROTATE ? rotated<BF16>(p, head, d0 + e, pos) : act_to_f32<BF16>(head[d0 + e]);
+    return;
+  }
+  float a[8], b[8];
+  const uint4* at = reinterpret_cast<const uint4*>(head + d0);
+  unpack8<BF16>(at[0], a); unpack8<BF16>(at[1], b);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) { x[e] = a[e]; x[8 + e] = b[e]; }
+  if (!ROTATE || d0 >= p.rot) return;
+  const int half = p.rot / 2;
+  if (p.neighbours) {
+    const float4* c = reinterpret_cast<const float4*>(p.cos + pos * half + d0 / 2);
+    const float4* s = reinterpret_cast<const float4*>(p.sin + pos * half + d0 / 2);
+    float cs[8], sn[8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float4 u = c[i], v = s[i];
+      cs[4 * i] = u.x; cs[4 * i + 1] = u.y; cs[4 * i + 2] = u.z; cs[4 * i + 3] = u.w;
+      sn[4 * i] = v.x; sn[4 * i + 1] = v.y; sn[4 * i + 2] = v.z; sn[4 * i + 3] = v.w;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float u = x[2 * e], v = x[2 * e + 1];
+      x[2 * e] = __fsub_rn(__fmul_rn(u, cs[e]), __fmul_rn(v, sn[e]));
+      x[2 * e + 1] = __fadd_rn(__fmul_rn(v, cs[e]), __fmul_rn(u, sn[e]));
+    }
+  } else {
+    const bool second = d0 >= half;
+    const int pair = second ? d0 - half : d0;
+    float y[16];
+    at = reinterpret_cast<const uint4*>(head + (second ? d0 - half : d0 + half));
+    unpack8<BF16>(at[0], a); unpack8<BF16>(at[1], b);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { y[e] = a[e]; y[8 + e] = b[e]; }
+    const float4* c = reinterpret_cast<const float4*>(p.cos + pos * half + pair);
+    const float4* s = reinterpret_cast<const float4*>(p.sin + pos * half + pair);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 u = c[i], v = s[i];
+      const float cs[4] = {u.x, u.y, u.z, u.w}, sn[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float own = __fmul_rn(x[4 * i + e], cs[e]), other = __fmul_rn(y[4 * i + e], sn[e]);
+        x[4 * i + e] = second ? __fadd_rn(own, other) : __fsub_rn(own, other);
+      }
+    }
+  }
+}
+
+template <bool E4M3>
+__device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float d) {
+  if constexpr (E4M3) return codes_e4m3(a, b, c, d);
+  else                return codes_i8(a, b, c, d) ^ 0x80808080u;       // offset-binary
+}
+template <bool E4M3>
+__device__ __forceinline__ void four_numbers(uint32_t u, float (&x)[4]) {
+  if constexpr (E4M3) {
+    x[0] = __builtin_amdgcn_cvt_f32_fp8((int)u, 0); x[1] = __builtin_amdgcn_cvt_f32_fp8((int)u, 1);
+    x[2] = __builtin_amdgcn_cvt_f32_fp8((int)u, 2); x[3] = __builtin_amdgcn_cvt_f32_fp8((int)u, 3);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = (float)((u >> (8 * e)) & 255u) - 128.0f;
+  }
+}
+
+// Queries: a workgroup per row.
+template <int D, bool BF16>
+__device__ __forceinline__ void rotate_queries(const KvParams& p, int row, int l) {
+  const int b = find_sequence(p, row, l);
+  if (b < 0) return;
+  const Sequence s = sequence(p, b);
+  if (row < s.first || row - s.first >= s.rows) return;
+  const int64_t pos = min(max((int64_t)s.before + (row - s.first), (int64_t)0), max(p.positions - 1, (int64_t)0));
+  const int pieces = p.q_heads * (D / 16);
+  for (int i = threadIdx.x; i < pieces; i += KV_THREADS) {
+    // partners are read before anything of the head is written: the output may be the input
+    float x[16];
+    const uint16_t* head = p.q + (int64_t)row * p.q_stride + (i / (D / 16)) * D;
+    if (p.cos) sixteen<BF16, true>(p, head, (i % (D / 16)) * 16, pos, x);
+    else       sixteen<BF16, false>(p, head, (i % (D / 16)) * 16, pos, x);
+    float a[8], c[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { a[e] = x[e]; c[e] = x[8 + e]; }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    uint4* out = reinterpret_cast<uint4*>(p.q_out + ((int64_t)row * p.q_heads * D + i * 16));
+    out[0] = pack8<BF16>(a); out[1] = pack8<BF16>(c);
+  }
+}
+
+template <int D, bool BF16, bool E4M3>
+__global__ __launch_bounds__(KV_THREADS) void append_kernel(KvParams p, int kv_units) {
+  constexpr int BYTES = KV_BLOCK * D, PER = BYTES / 16 / KV_THREADS;         // pieces of 16 elements a thread
+  constexpr float QMAX = E4M3 ? 448.0f : 127.0f;
+  __shared__ __attribute__((aligned(16))) uint8_t image[BYTES];              // the block as it lies in the cache
+  __shared__ uint32_t most[KV_THREADS / 64];
+  const int tid = threadIdx.x, l = tid & 63;
+  int unit = blockIdx.x;
+  if (unit >= kv_units) { rotate_queries<D, BF16>(p, unit - kv_units, l); return; }
+  const bool values = unit & 1;
+  const int head = (unit >> 1) % p.kv_heads;
+  int nth;
+  const int b = find_unit(p, (unit >> 1) / p.kv_heads, l, &nth);
+  if (b < 0) return;
+  const Sequence s = sequence(p, b);
+  const Touched t = touched(p, s);
+  if (nth >= t.count) return;
+  const int block = t.first + nth;
+  const uint32_t id = (uint32_t)p.table[b * p.width + block];
+  if (id >= (uint64_t)p.num_blocks) return;
+  const int from = max(t.from - block * KV_BLOCK, 0), upto = min(t.upto - block * KV_BLOCK, KV_BLOCK);     // the new tokens
+  float* scale_at = (values ? p.v_scale : p.k_scale) + (int64_t)id * p.kv_heads + head;
+  uint8_t* cache = (values ? p.v_cache : p.k_cache) + ((int64_t)id * p.kv_heads + head) * BYTES;
+  const float was = from > 0 ? *scale_at : 0.0f;
+
+  // the new values of this thread, and the largest of all
+  float x[PER][16];
+  uint32_t amax = 0u;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int piece = tid + i * KV_THREADS, token = piece / (D / 16), d0 = piece % (D / 16) * 16;
+    if (token < from || token >= upto) continue;
+    const int pos = block * KV_BLOCK + token;
+    const int64_t row = s.first + (pos - s.before);
+    if (values) sixteen<BF16, false>(p, p.v + row * p.v_stride + head * D, d0, 0, x[i]);
+    else if (p.cos) sixteen<BF16, true>(p, p.k + row * p.k_stride + head * D, d0, min((int64_t)pos, p.positions - 1), x[i]);
+    else sixteen<BF16, false>(p, p.k + row * p.k_stride + head * D, d0, 0, x[i]);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) amax = max(amax, magnitude(x[i][e]));
+  }
+#pragma unroll
+  for (int m = 32; m > 0; m >>= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, m));
+  if (l == 0) most[tid >> 6] = amax;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < KV_THREADS / 64; ++i) amax = max(amax, most[i]);
+  float scale = scale_of(amax, QMAX);
+  if (from > 0 && !(scale > was) && scale == scale) scale = was;             // also where what was there is NaN
+  if (from > 0 && was != was) scale = was;
+  const float inv = 1.0f / scale;
+
+  // few tokens into a block whose scale stays: just their bytes.  Otherwise the block is put together in LDS and written whole,
+  // with zeros for the tokens to come
+  const bool whole = from == 0 || scale != was;
+  if (whole && from > 0) {
+    const float move = was * inv;
+    for (int i = tid; i < BYTES / 16; i += KV_THREADS) {
+      uint4 c = reinterpret_cast<const uint4*>(cache)[i];
+      uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float y[4];
+        four_numbers<E4M3>(w[e], y);
+        w[e] = four_codes<E4M3>(y[0] * move, y[1] * move, y[2] * move, y[3] * move);
+      }
+      reinterpret_cast<uint4*>(image)[i] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __syncthreads();
+  } else if (whole) {
+    const uint32_t none = E4M3 ? 0u : 0x80808080u;
+    for (int i = tid; i < BYTES / 16; i += KV_THREADS) reinterpret_cast<uint4*>(image)[i] = make_uint4(none, none, none, none);
+    __syncthreads();
+  }
+  uint8_t* to = whole ? image : cache;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int piece = tid + i * KV_THREADS, token = piece / (D / 16), d0 = piece % (D / 16) * 16;
+    if (token < from || token >= upto) continue;
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      w[e] = four_codes<E4M3>(x[i][4 * e] * inv, x[i][4 * e + 1] * inv, x[i][4 * e + 2] * inv, x[i][4 * e + 3] * inv);
+    if (!values) {
+      *reinterpret_cast<uint4*>(to + key_byte<D>(token, d0)) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) to[value_byte(token, d0 + e)] = (uint8_t)(w[e / 4] >> (8 * (e % 4)));
+    }
+  }
+  if (whole) {
+    __syncthreads();
+    for (int i = tid; i < BYTES / 16; i += KV_THREADS) reinterpret_cast<uint4*>(cache)[i] = reinterpret_cast<const uint4*>(image)[i];
+    if (tid == 0) *scale_at = scale;
+  }
+}
+
+// The values of the last rows of each sequence.  A block's bytes go through LDS: they are read in their order and
+// written in the rows'.
+template <int D, bool BF16, bool E4M3>
+__global__ __launch_bounds__(KV_THREADS) void dequant_kernel_kv(KvParams p) {
+  constexpr int BYTES = KV_BLOCK * D;
+  __shared__ __attribute__((aligned(16))) uint8_t image[BYTES];
+  const int tid = threadIdx.x, l = tid & 63, unit = blockIdx.x;
+  const bool values = unit & 1;
+  const int head = (unit >> 1) % p.kv_heads;
+  int nth;
+  const int b = find_unit(p, (unit >> 1) / p.kv_heads, l, &nth);
+  if (b < 0) return;
+  const Sequence s = sequence(p, b);
+  const Touched t = touched(p, s);
+  if (nth >= t.count) return;
+  const int block = t.first + nth;
+  const uint32_t id = (uint32_t)p.table[b * p.width + block];
+  const bool there = id < (uint64_t)p.num_blocks;
+  float scale = 0.0f;
+  if (there) {
+    scale = (values ? p.v_scale : p.k_scale)[(int64_t)id * p.kv_heads + head];
+    const uint8_t* cache = (values ? p.v_cache : p.k_cache) + ((int64_t)id * p.kv_heads + head) * BYTES;
+    for (int i = tid; i < BYTES / 16; i += KV_THREADS) reinterpret_cast<uint4*>(image)[i] = reinterpret_cast<const uint4*>(cache)[i];
+  }
+  __syncthreads();
+  const int from = max(t.from - block * KV_BLOCK, 0), upto = min(t.upto - block * KV_BLOCK, KV_BLOCK);
+  uint16_t* out = values ? p.v_out : p.k_out;
+  for (int i = tid; i < BYTES / 8; i += KV_THREADS) {
+    const int token = i / (D / 8), d0 = i % (D / 8) * 8;
+    if (token < from || token >= upto) continue;
+    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (there) {
+      uint32_t w[2];
+      if (values) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          w[e] = image[value_byte(token, d0 + 4 * e)] | image[value_byte(token, d0 + 4 * e + 1)] << 8 |
+                 image[value_byte(token, d0 + 4 * e + 2)] << 16 | (uint32_t)image[value_byte(token, d0 + 4 * e + 3)] << 24;
+      } else {
+        const uint2 u = *reinterpret_cast<const uint2*>(image + key_byte<D>(token, d0));
+        w[0] = u.x; w[1] = u.y;
+      }
+      float y[4];
+      four_numbers<E4M3>(w[0], y);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = y[e] * scale;
+      four_numbers<E4M3>(w[1], y);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[4 + e] = y[e] * scale;
+    }
+    const int64_t row = s.first + (block * KV_BLOCK + token - s.before);
+    *reinterpret_cast<uint4*>(out + (row * p.kv_heads + head) * D + d0) = pack8<BF16>(x);
+  }
+}
+
+template <int D, bool BF16, bool E4M3>
+static int launch_append(const KvParams& p, hipStream_t st) {
+  const int64_t units = most_units(p) * p.kv_heads * 2, grid = units + (p.q ? p.rows : 0);
+  if (grid == 0) return QG_OK;
+  if (grid > MOST_GROUPS) return QG_EUNSUPPORTED;
+  hipLaunchKernelGGL((append_kernel<D, BF16, E4M3>), dim3((unsigned)grid), dim3(KV_THREADS), 0, st, p, (int)units);
+  return hipGetLastError() == hipSuccess ? QG_OK : QG_EHIP;
+}
+template <int D, bool BF16, bool E4M3>
+static int launch_dequant(const KvParams& p, hipStream_t st) {
+  const int64_t units = most_units(p) * p.kv_heads * 2;
+  if (units == 0) return QG_OK;
+  if (units > MOST_GROUPS) return QG_EUNSUPPORTED;
+  hipLaunchKernelGGL((dequant_kernel_kv<D, BF16, E4M3>), dim3((unsigned)units), dim3(KV_THREADS), 0, st, p);
+  return hipGetLastError() == hipSuccess ? QG_OK : QG_EHIP;
+}
+
+#define QG_KV_CHOOSE(fn)                                                                            \
+  const int which = (head_dim == 128 ? 4 : 0) + (p.bf16 ? 2 : 0) + (p.e4m3 ? 1 : 0);                \
+  switch (which) {                                                                                  \
+    case 0: return fn<64, false, false>(p, st);                                                     \
+    case 1: return fn<64, false, true>(p, st);                                                      \
+    case 2: return fn<64, true, false>(p, st);                                                      \
+    case 3: return fn<64, true, true>(p, st);                                                       \
+    case 4: return fn<128, false, false>(p, st);                                                    \
+    case 5: return fn<128, false, true>(p, st);                                                     \
+    case 6: return fn<128, true, false>(p, st);                                                     \
+    default: return fn<128, true, true>(p, st);                                                     \
+  }
+int kv_append_launch(const KvParams& p, int head_dim, hipStream_t st) { QG_KV_CHOOSE(launch_append) }
+int kv_dequant_launch(const KvParams& p, int head_dim, hipStream_t st) { QG_KV_CHOOSE(launch_dequant) }
+
+}  // namespace qg

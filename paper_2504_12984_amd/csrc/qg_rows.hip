@@ -1,0 +1,192 @@
+// Rows to 8 bits: the root-mean-square norm with the residual's addition, and the gated activation.
+//
+//   norm:  h = x + residual,  y = h * w / sqrt(mean(h^2) + eps)          gate:  y = g / (1 + exp(-g)) * u
+//   both:  a_scale = max(amax(y) / 127, 2^-40),  A8 = rne(y / a_scale)
+//
+// Bound: HBM (norm: 7 bytes an element with the residual, gate: 5).  A row is read once and stays in registers between the
+// reduction and the rounding.  The norm needs one reduction and not two: y's largest magnitude is that of h * w times the
+// factor that the sum of squares gives, so both are reduced together.
+#include "qg_layer.h"
+
+namespace qg {
+
+constexpr int OP_NORM = 0, OP_GATE = 1;
+
+// v_exp_f32 and v_rcp_f32 are good to about an ulp (and to |g| 2^-24 in the exponent, where the product is small): far below
+// the step of the codes.  1 + exp(-g) = infinity gives 0.
+__device__ __forceinline__ float silu_times(float g, float u) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u; }
+
+// What a row's reduction needs: sum of squares (norm) and the largest magnitude.
+struct RowSums { float sq; uint32_t amax; };
+template <int OP>
+__device__ __forceinline__ void wave_sums(RowSums& s) {
+#pragma unroll
+  for (int m = 32; m > 0; m >>= 1) {
+    if constexpr (OP == OP_NORM) s.sq += __shfl_xor(s.sq, m);
+    s.amax = max(s.amax, (uint32_t)__shfl_xor((int)s.amax, m));
+  }
+}
+// Over the W wavefronts of the workgroup; sums of wavefronts are added in their order.
+template <int OP, int W>
+__device__ __forceinline__ void row_sums(RowSums& s, int wave, int l) {
+  wave_sums<OP>(s);
+  if constexpr (W > 1) {
+    __shared__ float sq[W];
+    __shared__ uint32_t mx[W];
+    if (l == 0) { sq[wave] = s.sq; mx[wave] = s.amax; }
+    __syncthreads();
+    s.sq = 0.0f; s.amax = 0u;
+#pragma unroll
+    for (int i = 0; i < W; ++i) { s.sq += sq[i]; s.amax = max(s.amax, mx[i]); }
+  }
+}
+
+// From the reduction to the factor that takes a kept number (norm: h * w, gate: y) to its code.
+template <int OP>
+__device__ __forceinline__ float finish(const RowsParams& p, const RowSums& s, float* scale) {
+  float r = 1.0f;
+  uint32_t amax = s.amax;
+  if constexpr (OP == OP_NORM) {
+    r = 1.0f / sqrtf(s.sq / (float)p.N + p.eps);
+    amax = magnitude(__builtin_bit_cast(float, amax) * r);
+  }
+  *scale = scale_of(amax, 127.0f);
+  return r * (1.0f / *scale);
+}
+
+// Eight elements of a row: kept numbers in v, their part of the sums added, the rounded sum in `sum`.
+template <int OP, bool BF16>
+__device__ __forceinline__ void eight(const RowsParams& p, uint4 a, uint4 b, uint4 w, float (&v)[8], RowSums& s, uint4* sum) {
+  float y[8];
+  unpack8<BF16>(a, v);
+  if constexpr (OP == OP_NORM) {
+    if (p.y) {
+      unpack8<BF16>(b, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += y[e];
+    }
+    if (p.sum) *sum = pack8<BF16>(v);
+    unpack8<BF16>(w, y);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      s.sq = fmaf(v[e], v[e], s.sq);
+      v[e] *= y[e];
+      s.amax = max(s.amax, magnitude(v[e]));
+    }
+  } else {
+    unpack8<BF16>(b, y);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = silu_times(v[e], y[e]);
+      s.amax = max(s.amax, magnitude(v[e]));
+    }
+  }
+}
+
+// One row per W wavefronts, V vectors of 8 elements per lane, all in registers (N <= 512 * W * V, a multiple of 8; everything
+// aligned to 16 bytes).  W = 1: four rows to a workgroup, and no barrier.
+template <int OP, bool BF16, int W, int V>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rows_kernel(RowsParams p) {
+  const int l = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t row = W == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
+  if (W == 1 && row >= p.M) return;
+  const int tid = W == 1 ? l : threadIdx.x, vecs = p.N / 8;
+  const uint4* x = reinterpret_cast<const uint4*>(p.x + row * p.x_stride);
+  const uint4* y = reinterpret_cast<const uint4*>(p.y + row * p.y_stride);
+  uint4 a[V], b[V], w[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int at = tid + i * 64 * W;
+    a[i] = b[i] = w[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (at < vecs) {
+      a[i] = x[at];
+      if (OP == OP_GATE || p.y) b[i] = y[at];
+      if (OP == OP_NORM) w[i] = reinterpret_cast<const uint4*>(p.w)[at];
+    }
+  }
+  RowSums s = {0.0f, 0u};
+  float v[V][8];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    uint4 sum;
+    eight<OP, BF16>(p, a[i], b[i], w[i], v[i], s, &sum);
+    const int at = tid + i * 64 * W;
+    if (OP == OP_NORM && p.sum && at < vecs) reinterpret_cast<uint4*>(p.sum + row * p.sum_stride)[at] = sum;
+  }
+  row_sums<OP, W>(s, wave, l);
+  float scale;
+  const float f = finish<OP>(p, s, &scale);
+  if (tid == 0) p.a_scale[row] = scale;
+  uint2* out = reinterpret_cast<uint2*>(p.A8 + row * p.N);
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int at = tid + i * 64 * W;
+    if (at < vecs)
+      out[at] = make_uint2(codes_i8(v[i][0] * f, v[i][1] * f, v[i][2] * f, v[i][3] * f),
+                           codes_i8(v[i][4] * f, v[i][5] * f, v[i][6] * f, v[i][7] * f));
+  }
+}
+
+// Any width, any alignment: the row is read twice, element by element.  The sum is written on the second
+// reading, each element by the thread that reads it, so that it may replace an input.
+template <int OP, bool BF16>
+__global__ __launch_bounds__(1024) void rows_any_kernel(RowsParams p) {
+  const int l = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t row = blockIdx.x;
+  const uint16_t* x = p.x + row * p.x_stride;
+  const uint16_t* y = p.y + row * p.y_stride;
+  RowSums s = {0.0f, 0u};
+  const auto one = [&](int i, float* h) {
+    float v = act_to_f32<BF16>(x[i]);
+    if constexpr (OP == OP_GATE) return silu_times(v, act_to_f32<BF16>(y[i]));
+    if (p.y) v += act_to_f32<BF16>(y[i]);
+    *h = v;
+    return v * act_to_f32<BF16>(p.w[i]);
+  };
+  for (int i = threadIdx.x; i < p.N; i += 1024) {
+    float h = 0.0f;
+    s.amax = max(s.amax, magnitude(one(i, &h)));
+    s.sq = fmaf(h, h, s.sq);
+  }
+  row_sums<OP, 16>(s, wave, l);
+  float scale;
+  const float f = finish<OP>(p, s, &scale);
+  if (threadIdx.x == 0) p.a_scale[row] = scale;
+  for (int i = threadIdx.x; i < p.N; i += 1024) {
+    float h = 0.0f;
+    const float v = one(i, &h);
+    if (OP == OP_NORM && p.sum) p.sum[row * p.sum_stride + i] = f32_to_act<BF16>(h);
+    p.A8[row * p.N + i] = (int8_t)codes_i8(v * f, 0.0f, 0.0f, 0.0f);
+  }
+}
+
+template <int OP, bool BF16>
+static int launch_rows(const RowsParams& p, hipStream_t st) {
+  const int vecs = p.N / 8;
+#define QG_ROWS(W, V)                                                                                                    \
+  if (p.wide && vecs <= 64 * (W) * (V)) {                                                                                \
+    hipLaunchKernelGGL((rows_kernel<OP, BF16, W, V>), dim3((unsigned)((W) == 1 ? (p.M + 3) / 4 : p.M)),                  \
+                       dim3((W) == 1 ? 256 : 64 * (W)), 0, st, p);                                                       \
+    return hipGetLastError() == hipSuccess ? QG_OK : QG_EHIP;                                                            \
+  }
+  QG_ROWS(1, 1)
+  QG_ROWS(4, 1)
+  QG_ROWS(4, 2)
+  QG_ROWS(4, 4)
+  QG_ROWS(8, 4)
+  QG_ROWS(16, 4)
+#undef QG_ROWS
+  hipLaunchKernelGGL((rows_any_kernel<OP, BF16>), dim3((unsigned)p.M), dim3(1024), 0, st, p);
+  return hipGetLastError() == hipSuccess ? QG_OK : QG_EHIP;
+}
+
+int layer_norm_launch(const RowsParams& p, hipStream_t st) {
+  return p.bf16 ? launch_rows<OP_NORM, true>(p, st) : launch_rows<OP_NORM, false>(p, st);
+}
+int layer_gate_launch(const RowsParams& p, hipStream_t st) {
+  return p.bf16 ? launch_rows<OP_GATE, true>(p, st) : launch_rows<OP_GATE, false>(p, st);
+}
+
+}  // namespace qg
