@@ -45,6 +45,29 @@ __device__ __forceinline__ half8 numbers(uint32_t w0, uint32_t w1) {
   return half8{r[0][0], r[0][1], r[1][0], r[1][1], r[2][0], r[2][1], r[3][0], r[3][1]};
 }
 
+// Over the four lanes of a column (i, 16 + i, 32 + i, 48 + i), in all of them: swaps of rows of lanes, no trip through LDS.
+// (The results' elements are copied before their bits are cast: a cast of an element itself reads the first one.)
+template <class F>
+__device__ __forceinline__ float over_column(float x, F f) {
+  uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const uint32_t a0 = a[0], a1 = a[1];
+  u = __builtin_bit_cast(uint32_t, f(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1)));
+  const auto b = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t b0 = b[0], b1 = b[1];
+  return f(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
+}
+__device__ __forceinline__ float column_max(float x) { return over_column(x, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float column_sum(float x) { return over_column(x, [](float a, float b) { return a + b; }); }
+
+// Codes that one workgroup reads, once: past the caches.  (Not so where several workgroups read them, for different rows.)
+template <bool SHARED>
+__device__ __forceinline__ uint4 stream16(const uint4* at) {
+  if constexpr (SHARED) return *at;
+  typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u4*>(at)));
+}
+
 // What one block brings.
 struct BlockScales { float k, v; bool there; };
 
@@ -119,8 +142,7 @@ __device__ __forceinline__ float softmax_step(float4v (&acc)[4], half8 (&P)[2], 
   float top = NONE;
 #pragma unroll
   for (int t = 0; t < 4; ++t) top = fmaxf(top, fmaxf(fmaxf(acc[t][0], acc[t][1]), fmaxf(acc[t][2], acc[t][3])));
-  top = fmaxf(top, __shfl_xor(top, 16));
-  top = fmaxf(top, __shfl_xor(top, 32));
+  top = column_max(top);
   top = fmaf(top, f, lv);                                    // NaN (a scale, a score) never moves the reference
   float alpha = 1.0f;
   if (top > st.m + MOVE_BY) {
@@ -148,17 +170,17 @@ __device__ __forceinline__ float softmax_step(float4v (&acc)[4], half8 (&P)[2], 
 
 __device__ __forceinline__ uint32_t bytes_below(int n) { return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1u; }
 
-constexpr int STREAM_WAVES = 4, STREAM_ROWS = 16;
-// Partial results of one unit and part: O [16][D], then the 16 references and the 16 sums.
-template <int D>
-constexpr int PART = STREAM_ROWS * D + 2 * STREAM_ROWS;
+constexpr int STREAM_WAVES = 8;
+// Partial results of one unit and part: O [16 T][D], then the references and the sums of the 16 T rows.
+template <int D, int T>
+constexpr int PART = 16 * T * (D + 2);
 
-// Few rows per sequence: the cache is streamed once.  A workgroup takes 16 rows (query heads of one key/value head,
+// Few rows per sequence: the cache is streamed once.  A workgroup takes 16 T rows (query heads of one key/value head,
 // consecutive tokens) and a part of the blocks they see; its wavefronts take every fourth block each, all by themselves,
 // and meet at the end.  Bound: HBM, 2 D bytes a token and head.
-template <int D, bool BF16, bool E4M3>
+template <int D, bool BF16, bool E4M3, int T, bool SHARED>
 __global__ __launch_bounds__(64 * STREAM_WAVES, 2) void stream_kernel(KvParams p) {
-  constexpr int BYTES = KV_BLOCK * D, LOADS = BYTES / 1024;
+  constexpr int BYTES = KV_BLOCK * D, LOADS = BYTES / 1024, STREAM_ROWS = 16 * T;
   __shared__ __attribute__((aligned(16))) float o_sh[STREAM_WAVES][STREAM_ROWS][D + 4];
   __shared__ float m_sh[STREAM_WAVES][STREAM_ROWS], l_sh[STREAM_WAVES][STREAM_ROWS];
   __shared__ unsigned last;
@@ -182,64 +204,85 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, 2) void stream_kernel(KvParams p
   if (part >= parts) return;
   const int begin = first + part * each, end = min(begin + each, first + count);
 
-  const int row = r0 + i, pos = s.before + row / G;
-  const bool valid = row < rows;
-  Seen see = seen(p, pos, length);
-  if (!valid) see.lo = see.hi = 0;
-  half8 q[D / 32];
-  const uint16_t* q_row = valid ? p.q + (int64_t)(s.first + row / G) * p.q_stride + (h * G + row % G) * D : nullptr;
-  const float cs = load_q<D, BF16>(q_row, p.wide, b4, q) * p.factor;
+  half8 q[T][D / 32];
+  float cs[T];
+  Seen see[T];
+  RowState st[T];
+  float4v o[T][D / 16];
+#pragma unroll
+  for (int n = 0; n < T; ++n) {
+    const int row = r0 + 16 * n + i;
+    const bool valid = row < rows;
+    see[n] = seen(p, s.before + row / G, length);
+    if (!valid) see[n].lo = see[n].hi = 0;
+    const uint16_t* q_row = valid ? p.q + (int64_t)(s.first + row / G) * p.q_stride + (h * G + row % G) * D : nullptr;
+    cs[n] = load_q<D, BF16>(q_row, p.wide, b4, q[n]) * p.factor;
+    st[n] = {NONE, 0.0f};
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) o[n][d] = float4v{0, 0, 0, 0};
+  }
 
   const int32_t* table = p.table + (int64_t)b * p.width;
-  RowState st = {NONE, 0.0f};
-  float4v o[D / 16];
-#pragma unroll
-  for (int d = 0; d < D / 16; ++d) o[d] = float4v{0, 0, 0, 0};
   uint4 K[LOADS], V[LOADS];
   BlockScales bs;
   int64_t base;
-  const auto find = [&](int block) {
-    const uint32_t id = (uint32_t)table[block];
+  const auto find = [&](uint32_t id) {
     bs.there = id < (uint64_t)p.num_blocks;
     base = bs.there ? (int64_t)id * H + h : 0;
-    const float k = p.k_scale[base], v = p.v_scale[base];
-    bs.k = k; bs.v = v < SCALE_FLOOR ? SCALE_FLOOR : v;
+    bs.k = p.k_scale[base]; bs.v = p.v_scale[base];
   };
   const auto load_k = [&]() {
     const uint4* at = reinterpret_cast<const uint4*>(p.k_cache + base * BYTES) + l;
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) K[j] = at[64 * j];
+    for (int j = 0; j < LOADS; ++j) K[j] = stream16<SHARED>(at + 64 * j);
   };
   const auto load_v = [&]() {
     const uint4* at = reinterpret_cast<const uint4*>(p.v_cache + base * BYTES) + l;
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) V[j] = at[64 * j];
+    for (int j = 0; j < LOADS; ++j) V[j] = stream16<SHARED>(at + 64 * j);
   };
   int block = begin + wave;
-  if (block < end) { find(block); load_k(); load_v(); }
+  // where a block lies is read a turn ahead of its codes, its scales with them
+  uint32_t next_id = 0;
+  if (block < end) {
+    find((uint32_t)table[block]);
+    next_id = (uint32_t)table[min(block + STREAM_WAVES, end - 1)];
+    load_k();
+    __builtin_amdgcn_sched_barrier(0);       // keys first, here as in the loop: its waits count on the order
+    load_v();
+  }
   while (block < end) {
     const int next = block + STREAM_WAVES;
     const BlockScales now = bs;
-    float4v acc[4];
+    float4v acc[T][4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      acc[t] = float4v{0, 0, 0, 0};
+    for (int n = 0; n < T; ++n)
 #pragma unroll
-      for (int c = 0; c < D / 64; ++c) {
-        const uint4 w = K[t * (D / 64) + c];
-        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(numbers<E4M3>(w.x, w.y), q[2 * c], acc[t], 0, 0, 0);
-        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(numbers<E4M3>(w.z, w.w), q[2 * c + 1], acc[t], 0, 0, 0);
+      for (int t = 0; t < 4; ++t) acc[n][t] = float4v{0, 0, 0, 0};
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const uint4 w = K[t * (D / 64) + c / 2];
+        const half8 a = c % 2 ? numbers<E4M3>(w.z, w.w) : numbers<E4M3>(w.x, w.y);
+#pragma unroll
+        for (int n = 0; n < T; ++n) acc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, q[n][c], acc[n][t], 0, 0, 0);
       }
-    }
     // the next block's keys are on their way while this one's scores are worked on
-    if (next < end) { find(next); load_k(); }
-    const float f = cs * now.k, lv = __builtin_amdgcn_logf(now.v), ivs = 1.0f / now.v;
+    if (next < end) {
+      find(next_id);
+      next_id = (uint32_t)table[min(next + STREAM_WAVES, end - 1)];
+      load_k();
+    }
+    const float vs = now.v < SCALE_FLOOR ? SCALE_FLOOR : now.v;
+    const float lv = __builtin_amdgcn_logf(vs), ivs = 1.0f / vs;
     const int token0 = block * KV_BLOCK + 4 * b4;
     const bool edge = !now.there || block * KV_BLOCK < lo || block * KV_BLOCK + KV_BLOCK > hi;
-    half8 P[2];
-    float alpha;
+    half8 P[T][2];
+    float alpha[T];
     if (edge) {
-      alpha = softmax_step<true>(acc, P, st, f, lv, ivs, token0, now.there ? see : Seen{0, 0});
+#pragma unroll
+      for (int n = 0; n < T; ++n) alpha[n] = softmax_step<true>(acc[n], P[n], st[n], cs[n] * now.k, lv, ivs, token0, now.there ? see[n] : Seen{0, 0});
       // bytes of tokens that are not there may be anything, also NaN
       if constexpr (E4M3) {
         uint32_t keep[4];
@@ -249,30 +292,38 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, 2) void stream_kernel(KvParams p
         for (int j = 0; j < LOADS; ++j) { V[j].x &= keep[0]; V[j].y &= keep[1]; V[j].z &= keep[2]; V[j].w &= keep[3]; }
       }
     } else {
-      alpha = softmax_step<false>(acc, P, st, f, lv, ivs, token0, see);
-    }
-    if (__ballot(alpha != 1.0f)) {
 #pragma unroll
-      for (int d = 0; d < D / 16; ++d) o[d] *= alpha;
+      for (int n = 0; n < T; ++n) alpha[n] = softmax_step<false>(acc[n], P[n], st[n], cs[n] * now.k, lv, ivs, token0, see[n]);
     }
 #pragma unroll
-    for (int d = 0; d < D / 16; ++d) {
-      o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(numbers<E4M3>(V[d].x, V[d].y), P[0], o[d], 0, 0, 0);
-      o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(numbers<E4M3>(V[d].z, V[d].w), P[1], o[d], 0, 0, 0);
-    }
+    for (int n = 0; n < T; ++n)
+      if (__ballot(alpha[n] != 1.0f)) {
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) o[n][d] *= alpha[n];
+      }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) {
+        const half8 a = k ? numbers<E4M3>(V[d].z, V[d].w) : numbers<E4M3>(V[d].x, V[d].y);
+#pragma unroll
+        for (int n = 0; n < T; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, P[n][k], o[n][d], 0, 0, 0);
+      }
     if (next < end) load_v();
     block = next;
   }
 
   // the wavefronts meet
-  st.l += __shfl_xor(st.l, 16);
-  st.l += __shfl_xor(st.l, 32);
-  if (b4 == 0) { m_sh[wave][i] = st.m; l_sh[wave][i] = st.l; }
 #pragma unroll
-  for (int d = 0; d < D / 16; ++d) *reinterpret_cast<float4v*>(&o_sh[wave][i][16 * d + 4 * b4]) = o[d];
+  for (int n = 0; n < T; ++n) {
+    const float sum = column_sum(st[n].l);
+    if (b4 == 0) { m_sh[wave][16 * n + i] = st[n].m; l_sh[wave][16 * n + i] = sum; }
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) *reinterpret_cast<float4v*>(&o_sh[wave][16 * n + i][16 * d + 4 * b4]) = o[n][d];
+  }
   __syncthreads();
-  constexpr int PER = D / 16;                        // dimensions a thread
-  const int mine = tid / 16, d0 = (tid % 16) * PER, my_row = r0 + mine;
+  constexpr int EACH = 4 * STREAM_WAVES / T, PER = D / EACH;    // threads to a row, dimensions a thread
+  const int mine = tid / EACH, d0 = (tid % EACH) * PER, my_row = r0 + mine;
   float M = NONE, L = 0.0f, x[PER];
 #pragma unroll
   for (int w = 0; w < STREAM_WAVES; ++w) M = fmaxf(M, m_sh[w][mine]);
@@ -288,14 +339,14 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, 2) void stream_kernel(KvParams p
   if (parts > 1) {
     // parts meet in the workspace: device-scope relaxed stores are out when they are waited for, and the last one to come
     // adds all parts up in their order
-    float* to = p.partial + ((int64_t)blockIdx.x * gridDim.y + part) * PART<D>;
+    float* to = p.partial + ((int64_t)blockIdx.x * gridDim.y + part) * PART<D, T>;
     if (my_row < rows) {
 #pragma unroll
       for (int e = 0; e < PER; e += 2) {
         const uint64_t two = __builtin_bit_cast(uint32_t, x[e]) | (uint64_t)__builtin_bit_cast(uint32_t, x[e + 1]) << 32;
         __hip_atomic_store(reinterpret_cast<unsigned long long*>(to + mine * D + d0 + e), two, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
-      if (tid % 16 == 0) {
+      if (tid % EACH == 0) {
         __hip_atomic_store(to + STREAM_ROWS * D + mine, M, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __hip_atomic_store(to + STREAM_ROWS * D + STREAM_ROWS + mine, L, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
@@ -308,34 +359,60 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, 2) void stream_kernel(KvParams p
     if (!last) return;
     if (tid == 0) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (my_row >= rows) return;
-    const float* of = p.partial + (int64_t)blockIdx.x * gridDim.y * PART<D>;
+    const float* of = p.partial + (int64_t)blockIdx.x * gridDim.y * PART<D, T>;
+    const auto stat = [&](int k, int which) {
+      return __hip_atomic_load(of + k * PART<D, T> + STREAM_ROWS * (D + which) + mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    };
+    // A turn to AHEAD parts, all of whose loads are under way together.  (The last turn's loads past the end read
+    // the last part again and count for nothing.)
+    constexpr int AHEAD = 8;
     M = NONE;
-    for (int k = 0; k < parts; ++k)
-      M = fmaxf(M, __hip_atomic_load(of + k * PART<D> + STREAM_ROWS * D + mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
     L = 0.0f;
 #pragma unroll
     for (int e = 0; e < PER; ++e) x[e] = 0.0f;
-    for (int k = 0; k < parts; ++k) {
-      const float* at = of + k * PART<D>;
-      const float m = __hip_atomic_load(at + STREAM_ROWS * D + mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      const float a = M == NONE ? 1.0f : __builtin_amdgcn_exp2f(m - M);
-      L = fmaf(a, __hip_atomic_load(at + STREAM_ROWS * D + STREAM_ROWS + mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), L);
+    for (int k0 = 0; k0 < parts; k0 += AHEAD) {
+      float m[AHEAD], sum[AHEAD];
+      uint64_t two[AHEAD][PER / 2];
 #pragma unroll
-      for (int e = 0; e < PER; e += 2) {
-        const uint64_t two = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(at + mine * D + d0 + e), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        x[e] = fmaf(a, __builtin_bit_cast(float, (uint32_t)two), x[e]);
-        x[e + 1] = fmaf(a, __builtin_bit_cast(float, (uint32_t)(two >> 32)), x[e + 1]);
+      for (int k = 0; k < AHEAD; ++k) {
+        const int part_k = min(k0 + k, parts - 1);
+        m[k] = stat(part_k, 0);
+        sum[k] = stat(part_k, 1);
+#pragma unroll
+        for (int e = 0; e < PER / 2; ++e)
+          two[k][e] = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(of + part_k * PART<D, T> + mine * D + d0 + 2 * e), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+      float top = M;
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) top = fmaxf(top, m[k]);
+      const float back = top == NONE ? 1.0f : __builtin_amdgcn_exp2f(M - top);
+      M = top;
+      L *= back;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) x[e] *= back;
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        float a = M == NONE ? 1.0f : __builtin_amdgcn_exp2f(m[k] - M);
+        if (k0 + k >= parts) { a = 0.0f; sum[k] = 0.0f; }
+        L = fmaf(a, sum[k], L);
+#pragma unroll
+        for (int e = 0; e < PER / 2; ++e) {
+          const uint64_t u = k0 + k < parts ? two[k][e] : 0;
+          x[2 * e] = fmaf(a, __builtin_bit_cast(float, (uint32_t)u), x[2 * e]);
+          x[2 * e + 1] = fmaf(a, __builtin_bit_cast(float, (uint32_t)(u >> 32)), x[2 * e + 1]);
+        }
       }
     }
   }
   if (my_row >= rows) return;
   const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-  uint32_t w[PER / 2];
+  uint32_t w[PER / 2 > 0 ? PER / 2 : 1];
 #pragma unroll
   for (int e = 0; e < PER; e += 2) w[e / 2] = pack2<BF16>(x[e] * inv, x[e + 1] * inv);
   uint16_t* out = p.out + ((int64_t)(s.first + my_row / G) * p.q_heads + h * G + my_row % G) * D + d0;
-  if constexpr (PER == 8) *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
-  else                    *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
+  if constexpr (PER == 8)      *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
+  else if constexpr (PER == 4) *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
+  else                         *reinterpret_cast<uint32_t*>(out) = w[0];
 }
 
 // Many rows per sequence: bound by the matrix instruction and the softmax's vector work.  A workgroup takes 256 rows (the
@@ -463,9 +540,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES) void tile_kernel(KvParams p) {
 #pragma unroll
   for (int n = 0; n < TILE_QT; ++n) {
     const int row = w0 + 16 * n + i;
-    float L = st[n].l;
-    L += __shfl_xor(L, 16);
-    L += __shfl_xor(L, 32);
+    const float L = column_sum(st[n].l);
     const float inv = L == 0.0f ? 0.0f : 1.0f / L;
     if (row >= rows) continue;
     uint16_t* out = p.out + ((int64_t)(s.first + row / G) * p.q_heads + h * G + row % G) * D + 4 * b4;
@@ -473,6 +548,33 @@ __global__ __launch_bounds__(64 * TILE_WAVES) void tile_kernel(KvParams p) {
     for (int d = 0; d < D / 16; ++d)
       *reinterpret_cast<uint2*>(out + 16 * d) = make_uint2(pack2<BF16>(o[n][d][0] * inv, o[n][d][1] * inv), pack2<BF16>(o[n][d][2] * inv, o[n][d][3] * inv));
   }
+}
+
+// How long a part is.  Workgroups read at some 40 GB/s each, so as many as there are CUs stream the cache at its rate, and more
+// only add partial results; parts of less than four blocks do not pay for their meeting, and parts of at most 128 keep one
+// long sequence among short ones from being the last one left.  One row tile, 64 heads over 8, us:
+//   1 x 131071 tokens (8 units): 32 / 64 / 128 blocks 55 / 48 / 53;    64 x 1000 .. 8000 (512 units): 108.. for 128, 114 for 64, 119 for 32
+//   8 x 500 .. 4000 (64 units):  8 / 16 / 32 blocks 17 / 13 / 17;      1 x 1000 (8 units): 4 / 8 / 16 blocks 7.6 / 8.8 / 8.8
+template <int D, bool BF16, bool E4M3, int T>
+static int launch_stream(KvParams& p, int64_t max_tile_rows, int64_t max_kv, hipStream_t st) {
+  const int64_t tiles = (max_tile_rows + 16 * T - 1) / (16 * T), units = tiles * p.kv_heads * p.batch;
+  if (units > MOST_GROUPS) return QG_EUNSUPPORTED;
+  const int64_t blocks = std::max<int64_t>((max_kv + KV_BLOCK - 1) / KV_BLOCK, 1);
+  const size_t part = PART<D, T> * sizeof(float);
+  int64_t chunk = std::clamp<int64_t>((units * blocks + 255) / 256, 4, 128);
+  while (chunk < blocks && (size_t)units * ((blocks + chunk - 1) / chunk) * part > layer_workspace_bytes()) chunk *= 2;
+  int64_t parts = (blocks + chunk - 1) / chunk;
+  p.tiles = ticket_stride(units);
+  if (parts > 1 && (parts > 65535 || p.tiles * units > WS_TICKETS ||
+                    layer_workspace((size_t)units * parts * part, (size_t)(units * p.tiles), st, &p.partial, &p.tickets) != QG_OK)) {
+    parts = 1;
+    chunk = blocks;
+  }
+  p.splits = (int)std::min<int64_t>(chunk, INT32_MAX / KV_BLOCK);
+  const dim3 grid((unsigned)units, (unsigned)parts), threads(64 * STREAM_WAVES);
+  if (tiles > 1) hipLaunchKernelGGL((stream_kernel<D, BF16, E4M3, T, true>), grid, threads, 0, st, p);
+  else           hipLaunchKernelGGL((stream_kernel<D, BF16, E4M3, T, false>), grid, threads, 0, st, p);
+  return hipGetLastError() == hipSuccess ? QG_OK : QG_EHIP;
 }
 
 template <int D, bool BF16, bool E4M3>
@@ -486,23 +588,8 @@ static int launch_attention(KvParams& p, int64_t max_kv, hipStream_t st) {
     hipLaunchKernelGGL((tile_kernel<D, BF16, E4M3>), dim3((unsigned)grid), dim3(64 * TILE_WAVES), 0, st, p);
     return hipGetLastError() == hipSuccess ? QG_OK : QG_EHIP;
   }
-  const int64_t tiles = (max_tile_rows + STREAM_ROWS - 1) / STREAM_ROWS, units = tiles * p.kv_heads * p.batch;
-  if (units > MOST_GROUPS) return QG_EUNSUPPORTED;
-  const int64_t blocks = std::max<int64_t>((max_kv + KV_BLOCK - 1) / KV_BLOCK, 1);
-  int64_t chunk = std::max<int64_t>((units * blocks + 2047) / 2048, 4);
-  const size_t part = PART<D> * sizeof(float);
-  chunk = std::max<int64_t>(chunk, 4);
-  while (chunk < blocks && (size_t)units * ((blocks + chunk - 1) / chunk) * part > layer_workspace_bytes()) chunk *= 2;
-  int64_t parts = (blocks + chunk - 1) / chunk;
-  if (parts > 1 && parts <= 65535) {
-    p.tiles = ticket_stride(units);
-    if ((int64_t)p.tiles * units > WS_TICKETS ||
-        layer_workspace((size_t)units * parts * part, (size_t)units * p.tiles, st, &p.partial, &p.tickets) != QG_OK) parts = 1;
-  }
-  if (parts == 1 || parts > 65535) { parts = 1; chunk = std::max<int64_t>(blocks, p.width); }
-  p.splits = (int)std::min<int64_t>(chunk, INT32_MAX / KV_BLOCK);
-  hipLaunchKernelGGL((stream_kernel<D, BF16, E4M3>), dim3((unsigned)units, (unsigned)parts), dim3(64 * STREAM_WAVES), 0, st, p);
-  return hipGetLastError() == hipSuccess ? QG_OK : QG_EHIP;
+  return max_tile_rows <= 16 ? launch_stream<D, BF16, E4M3, 1>(p, max_tile_rows, max_kv, st)
+                             : launch_stream<D, BF16, E4M3, 2>(p, max_tile_rows, max_kv, st);
 }
 
 int kv_attention_launch(KvParams& p, int head_dim, int64_t max_kv, hipStream_t st) {
