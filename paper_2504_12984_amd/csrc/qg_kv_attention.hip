@@ -21,6 +21,7 @@ namespace qg {
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
 
 constexpr float MOVE_BY = 8.0f;
 constexpr float NONE = -__builtin_inff();
@@ -48,16 +49,24 @@ __device__ __forceinline__ half8 numbers(uint32_t w0, uint32_t w1) {
 // Over the four lanes of a column (i, 16 + i, 32 + i, 48 + i), in all of them: swaps of rows of lanes, no trip through LDS.
 // (The results' elements are copied before their bits are cast: a cast of an element itself reads the first one.)
 template <class F>
-__device__ __forceinline__ float over_column(float x, F f) {
-  uint32_t u = __builtin_bit_cast(uint32_t, x);
+__device__ __forceinline__ float over_halves(float x, F f) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
   const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
   const uint32_t a0 = a[0], a1 = a[1];
-  u = __builtin_bit_cast(uint32_t, f(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1)));
+  return f(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1));
+}
+template <class F>
+__device__ __forceinline__ float over_column(float x, F f) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, over_halves(x, f));
   const auto b = __builtin_amdgcn_permlane16_swap(u, u, false, false);
   const uint32_t b0 = b[0], b1 = b[1];
   return f(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
 }
-__device__ __forceinline__ float column_max(float x) { return over_column(x, [](float a, float b) { return fmaxf(a, b); }); }
+// (The maximum that hands a NaN on: the other one has to quieten its operands first, an instruction each.)
+__device__ __forceinline__ float top_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float column_max(float x) { return over_column(x, top_of); }
+__device__ __forceinline__ float half_max(float x) { return over_halves(x, top_of); }
+__device__ __forceinline__ float half_sum(float x) { return over_halves(x, [](float a, float b) { return a + b; }); }
 __device__ __forceinline__ float column_sum(float x) { return over_column(x, [](float a, float b) { return a + b; }); }
 
 // Codes that one workgroup reads, once: past the caches.  (Not so where several workgroups read them, for different rows.)
@@ -80,92 +89,201 @@ __device__ __forceinline__ Seen seen(const KvParams& p, int pos, int length) {
   return s;
 }
 
-// Rows of q as the matrix instruction's column operand: lane 16 b + i holds dimensions 64 c + 16 b + 8 e + 0..7 of row i.
-// Returns what the row was divided by.
-template <int D, bool BF16>
-__device__ __forceinline__ float load_q(const uint16_t* row, bool wide, int b, half8 (&q)[D / 32]) {
-  float x[D / 32][8];
+// A row of q, as 16-bit numbers -> the column operands of the matrix instruction: register group j holds dimensions at(j) ..
+// at(j) + 7; `others` is the maximum over the lanes that hold the rest of the row.  Returns what the row was divided by.
+template <bool BF16, int N, class At, class Others>
+__device__ __forceinline__ float load_q(const uint16_t* row, bool wide, half8 (&q)[N], At at, Others others) {
+  float x[N][8];
 #pragma unroll
-  for (int c = 0; c < D / 64; ++c)
+  for (int j = 0; j < N; ++j) {
+    float (&y)[8] = x[j];
+    if (!row) {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int at = 64 * c + 16 * b + 8 * e;
-      float (&y)[8] = x[2 * c + e];
-      if (!row) {
+      for (int k = 0; k < 8; ++k) y[k] = 0.0f;
+    } else if (wide) {
+      unpack8<BF16>(*reinterpret_cast<const uint4*>(row + at(j)), y);
+    } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) y[k] = 0.0f;
-      } else if (wide) {
-        unpack8<BF16>(*reinterpret_cast<const uint4*>(row + at), y);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) y[k] = act_to_f32<BF16>(row[at + k]);
-      }
+      for (int k = 0; k < 8; ++k) y[k] = act_to_f32<BF16>(row[at(j) + k]);
     }
+  }
   float by = 1.0f, inv = 1.0f;
   if constexpr (BF16) {
     // bf16 numbers reach beyond fp16's: the row's largest is brought to 1 .. 2 (a power of two: nothing is lost down to
     // 2^-14 of it, and 2^-25 of it below)
     uint32_t amax = 0u;
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j)
+    for (int j = 0; j < N; ++j)
 #pragma unroll
       for (int k = 0; k < 8; ++k) amax = max(amax, magnitude(x[j][k]));
-    amax = max(amax, (uint32_t)__shfl_xor((int)amax, 16));
-    amax = max(amax, (uint32_t)__shfl_xor((int)amax, 32));
+    amax = others(amax);
     // (exponents 1 .. 253, so that both factors are normal numbers)
     const uint32_t e = min(max(amax >> 23, 1u), 253u);
     if (amax < NOT_FINITE) { by = __builtin_bit_cast(float, e << 23); inv = __builtin_bit_cast(float, (254u - e) << 23); }
   }
 #pragma unroll
-  for (int j = 0; j < D / 32; ++j)
+  for (int j = 0; j < N; ++j)
 #pragma unroll
     for (int k = 0; k < 8; ++k) q[j][k] = (_Float16)(x[j][k] * inv);
   return by;
 }
+// Lane 16 b + i of the 16x16x32 instruction: dimensions 64 c + 16 b + 8 e + 0..7 of row i.
+template <int D, bool BF16>
+__device__ __forceinline__ float load_q_flat(const uint16_t* row, bool wide, int b, half8 (&q)[D / 32]) {
+  return load_q<BF16>(row, wide, q, [b](int j) { return 64 * (j / 2) + 16 * b + 8 * (j % 2); }, [](uint32_t m) {
+    m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+    return max(m, (uint32_t)__shfl_xor((int)m, 32));
+  });
+}
+// Lane 32 h + i of the 32x32x16 instruction: dimensions 16 j + 8 h + 0..7 of row i.
+template <int D, bool BF16>
+__device__ __forceinline__ float load_q_tall(const uint16_t* row, bool wide, int h, half8 (&q)[D / 16]) {
+  return load_q<BF16>(row, wide, q, [h](int j) { return 16 * j + 8 * h; }, [](uint32_t m) { return max(m, (uint32_t)__shfl_xor((int)m, 32)); });
+}
 
-// One tile of 16 rows against the 64 tokens of a block: from score registers to the operand of the second product.
-// `acc` are the products of q and codes, f the factor of the scores, moved: the factor that the accumulators have to be
-// multiplied by (1: none).
+// One tile of 16 rows against the 64 tokens of a block, in two steps.  `acc` are the products of q and codes, f the factor of
+// the scores, lv the logarithm of the values' scale; token0 is the first token of the lane, 64 * block + 4 b.
 struct RowState { float m, l; };
-template <bool EDGE>
-__device__ __forceinline__ float softmax_step(float4v (&acc)[4], half8 (&P)[2], RowState& st, float f, float lv, float ivs, int token0, Seen see) {
-  // token0: the first token of the lane, 64 * block + 4 b
-  if constexpr (EDGE) {
+
+// What a row does not see is out of its scores.
+__device__ __forceinline__ void mask_scores(float4v (&acc)[4], int token0, Seen see) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+  for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int token = token0 + 16 * t + r;
-        if (token < see.lo || token >= see.hi) acc[t][r] = NONE;
-      }
-  }
-  float top = NONE;
+    for (int r = 0; r < 4; ++r) {
+      const int token = token0 + 16 * t + r;
+      if (token < see.lo || token >= see.hi) acc[t][r] = NONE;
+    }
+}
+__device__ __forceinline__ float top_score(const float4v (&acc)[4]) {
+  float top = top_of(top_of(acc[0][0], acc[0][1]), top_of(acc[0][2], acc[0][3]));
 #pragma unroll
-  for (int t = 0; t < 4; ++t) top = fmaxf(top, fmaxf(fmaxf(acc[t][0], acc[t][1]), fmaxf(acc[t][2], acc[t][3])));
-  top = column_max(top);
-  top = fmaf(top, f, lv);                                    // NaN (a scale, a score) never moves the reference
-  float alpha = 1.0f;
+  for (int t = 1; t < 4; ++t) top = top_of(top, top_of(top_of(acc[t][0], acc[t][1]), top_of(acc[t][2], acc[t][3])));
+  return top;
+}
+// The reference, from each lane's largest product: moved where one of a column's four lanes is MOVE_BY above it.  Returns
+// whether any is; then the accumulators have to be multiplied by alpha.
+template <class Column>
+__device__ __forceinline__ bool move_reference(float top, RowState& st, float f, float lv, float& alpha, Column column) {
+  top = fmaf(top, f, lv);                                    // NaN (a scale, a score) does not move it: the row is NaN
+  if (!__ballot(top > st.m + MOVE_BY)) return false;
+  top = column(top);
+  alpha = 1.0f;
   if (top > st.m + MOVE_BY) {
     alpha = st.m == NONE ? 0.0f : __builtin_amdgcn_exp2f(st.m - top);
     st.m = top;
     st.l *= alpha;
   }
-  const float c = lv - (st.m == NONE ? 0.0f : st.m);
+  return true;
+}
+
+// Four tokens' scores to P', c = lv - reference; returns their sum.
+template <bool EDGE>
+__device__ __forceinline__ float four_probabilities(const float4v& acc, half8& P, int at, float f, float c, int token, Seen see) {
+  float e[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    e[r] = __builtin_amdgcn_exp2f(fmaf(acc[r], f, c));
+    if (EDGE && (token + r < see.lo || token + r >= see.hi)) e[r] = 0.0f;       // also where the block's scales are NaN
+    P[at + r] = (_Float16)e[r];
+  }
+  return (e[0] + e[1]) + (e[2] + e[3]);
+}
+__device__ __forceinline__ float exponent_constant(const RowState& st, float lv) { return lv - (st.m == NONE ? 0.0f : st.m); }
+__device__ __forceinline__ void add_sum(RowState& st, float sum, float ivs) { st.l += sum == 0.0f ? 0.0f : sum * ivs; }
+
+template <bool EDGE>
+__device__ __forceinline__ void probabilities(const float4v (&acc)[4], half8 (&P)[2], RowState& st, float f, float lv, float ivs, int token0, Seen see) {
+  const float c = exponent_constant(st, lv);
   float sum = 0.0f;
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
+  for (int t = 0; t < 4; ++t) sum += four_probabilities<EDGE>(acc[t], P[t / 2], 4 * (t % 2), f, c, token0 + 16 * t, see);
+  add_sum(st, sum, ivs);
+}
+// The same number, unknown to the compiler: what is computed from it stays in the branch that asks for it.
+__device__ __forceinline__ int hidden(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+// All of it, for T tiles and their accumulators o.  edge: some row does not see some token.
+template <int T, int N>
+__device__ __forceinline__ void softmax_step(float4v (&acc)[T][4], half8 (&P)[T][2], float4v (&o)[T][N], RowState (&st)[T], const float (&cs)[T],
+                                             const Seen (&see)[T], const BlockScales& block, bool edge, int token0) {
+  const float vs = block.v < SCALE_FLOOR ? SCALE_FLOOR : block.v;
+  const float lv = __builtin_amdgcn_logf(vs), ivs = 1.0f / vs;
+  Seen my[T];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float e = __builtin_amdgcn_exp2f(fmaf(acc[t][r], f, c));
-      if constexpr (EDGE) {
-        const int token = token0 + 16 * t + r;
-        if (token < see.lo || token >= see.hi) e = 0.0f;     // also where the block's scales are NaN
-      }
-      sum += e;
-      P[t / 2][4 * (t % 2) + r] = (_Float16)e;
+  for (int n = 0; n < T; ++n) my[n] = block.there ? see[n] : Seen{0, 0};
+  if (edge) {
+    const int token = hidden(token0);
+#pragma unroll
+    for (int n = 0; n < T; ++n) mask_scores(acc[n], token, my[n]);
+  }
+#pragma unroll
+  for (int n = 0; n < T; ++n) {
+    float alpha;
+    if (move_reference(top_score(acc[n]), st[n], cs[n] * block.k, lv, alpha, column_max)) {
+#pragma unroll
+      for (int d = 0; d < N; ++d) o[n][d] *= alpha;
     }
-  st.l += sum == 0.0f ? 0.0f : sum * ivs;
-  return alpha;
+  }
+  if (edge) {
+    const int token = hidden(token0);
+#pragma unroll
+    for (int n = 0; n < T; ++n) probabilities<true>(acc[n], P[n], st[n], cs[n] * block.k, lv, ivs, token, my[n]);
+  } else {
+#pragma unroll
+    for (int n = 0; n < T; ++n) probabilities<false>(acc[n], P[n], st[n], cs[n] * block.k, lv, ivs, token0, my[n]);
+  }
+}
+
+// The same for the 32 scores that a lane has with the 32x32x16 instruction: register r of tile k is token
+// token0 + 32 k + 8 (r / 4) + r % 4.
+__device__ __forceinline__ int tall_token(int k, int r) { return 32 * k + 8 * (r / 4) + r % 4; }
+template <bool EDGE>
+__device__ __forceinline__ void tall_probabilities(const float16v (&acc)[2], half8 (&P)[4], RowState& st, float f, float lv, float ivs, int token0, Seen see) {
+  const float c = exponent_constant(st, lv);
+  float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      float e = __builtin_amdgcn_exp2f(fmaf(acc[k][r], f, c));
+      if constexpr (EDGE) {
+        const int token = token0 + tall_token(k, r);
+        if (token < see.lo || token >= see.hi) e = 0.0f;      // also where the block's scales are NaN
+      }
+      sum[k] += e;
+      P[2 * k + r / 8][r % 8] = (_Float16)e;
+    }
+  add_sum(st, sum[0] + sum[1], ivs);
+}
+template <int N>
+__device__ __forceinline__ void tall_softmax_step(float16v (&acc)[2], half8 (&P)[4], float16v (&o)[N], RowState& st, float cs, Seen see,
+                                                  const BlockScales& block, bool edge, int token0) {
+  const float vs = block.v < SCALE_FLOOR ? SCALE_FLOOR : block.v;
+  const float lv = __builtin_amdgcn_logf(vs), ivs = 1.0f / vs, f = cs * block.k;
+  const Seen my = block.there ? see : Seen{0, 0};
+  if (edge) {
+    const int token1 = hidden(token0);
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int token = token1 + tall_token(k, r);
+        if (token < my.lo || token >= my.hi) acc[k][r] = NONE;
+      }
+  }
+  float top = top_of(acc[0][0], acc[1][0]);
+#pragma unroll
+  for (int r = 1; r < 16; ++r) top = top_of(top, top_of(acc[0][r], acc[1][r]));
+  float alpha;
+  if (move_reference(top, st, f, lv, alpha, half_max)) {
+#pragma unroll
+    for (int d = 0; d < N; ++d) o[d] *= alpha;
+  }
+  if (edge) tall_probabilities<true>(acc, P, st, f, lv, ivs, hidden(token0), my);
+  else      tall_probabilities<false>(acc, P, st, f, lv, ivs, token0, my);
 }
 
 __device__ __forceinline__ uint32_t bytes_below(int n) { return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1u; }
@@ -216,7 +334,7 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, 2) void stream_kernel(KvParams p
     see[n] = seen(p, s.before + row / G, length);
     if (!valid) see[n].lo = see[n].hi = 0;
     const uint16_t* q_row = valid ? p.q + (int64_t)(s.first + row / G) * p.q_stride + (h * G + row % G) * D : nullptr;
-    cs[n] = load_q<D, BF16>(q_row, p.wide, b4, q[n]) * p.factor;
+    cs[n] = load_q_flat<D, BF16>(q_row, p.wide, b4, q[n]) * p.factor;
     st[n] = {NONE, 0.0f};
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) o[n][d] = float4v{0, 0, 0, 0};
@@ -274,33 +392,17 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, 2) void stream_kernel(KvParams p
       next_id = (uint32_t)table[min(next + STREAM_WAVES, end - 1)];
       load_k();
     }
-    const float vs = now.v < SCALE_FLOOR ? SCALE_FLOOR : now.v;
-    const float lv = __builtin_amdgcn_logf(vs), ivs = 1.0f / vs;
     const int token0 = block * KV_BLOCK + 4 * b4;
     const bool edge = !now.there || block * KV_BLOCK < lo || block * KV_BLOCK + KV_BLOCK > hi;
     half8 P[T][2];
-    float alpha[T];
-    if (edge) {
+    softmax_step<T>(acc, P, o, st, cs, see, now, edge, token0);
+    if (E4M3 && edge) {      // bytes of tokens that are not there may be anything, also NaN
+      uint32_t keep[4];
 #pragma unroll
-      for (int n = 0; n < T; ++n) alpha[n] = softmax_step<true>(acc[n], P[n], st[n], cs[n] * now.k, lv, ivs, token0, now.there ? see[n] : Seen{0, 0});
-      // bytes of tokens that are not there may be anything, also NaN
-      if constexpr (E4M3) {
-        uint32_t keep[4];
+      for (int t = 0; t < 4; ++t) keep[t] = now.there ? bytes_below(length - (token0 + 16 * t)) : 0u;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) keep[t] = now.there ? bytes_below(length - (token0 + 16 * t)) : 0u;
-#pragma unroll
-        for (int j = 0; j < LOADS; ++j) { V[j].x &= keep[0]; V[j].y &= keep[1]; V[j].z &= keep[2]; V[j].w &= keep[3]; }
-      }
-    } else {
-#pragma unroll
-      for (int n = 0; n < T; ++n) alpha[n] = softmax_step<false>(acc[n], P[n], st[n], cs[n] * now.k, lv, ivs, token0, see[n]);
+      for (int j = 0; j < LOADS; ++j) { V[j].x &= keep[0]; V[j].y &= keep[1]; V[j].z &= keep[2]; V[j].w &= keep[3]; }
     }
-#pragma unroll
-    for (int n = 0; n < T; ++n)
-      if (__ballot(alpha[n] != 1.0f)) {
-#pragma unroll
-        for (int d = 0; d < D / 16; ++d) o[n][d] *= alpha[n];
-      }
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -415,16 +517,20 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, 2) void stream_kernel(KvParams p
   else                         *reinterpret_cast<uint32_t*>(out) = w[0];
 }
 
-// Many rows per sequence: bound by the matrix instruction and the softmax's vector work.  A workgroup takes 256 rows (the
-// query heads of one key/value head for 256 / heads consecutive tokens), 32 to a wavefront; a block's codes are
-// converted once for all of them, into LDS in the order in which lanes read operands.
-constexpr int TILE_WAVES = 8, TILE_QT = 2, TILE_ROWS = TILE_WAVES * TILE_QT * 16;
+// Many rows per sequence: bound by the vector work of the softmax and the matrix instruction, which takes 16 of 32 rows' cycles
+// from it.  A workgroup takes 256 rows (the query heads of one key/value head for consecutive tokens), 32 to a wavefront; a
+// block's codes are converted once for all of them, into LDS in the order in which lanes read operands.  Here the
+// matrix instruction is the 32x32x16 one: half as many of them issue, and a lane holds 32 scores of one row, so that there
+// is one reference and one sum to a lane.  Lane 32 h + i gets the scores of row i and tokens 32 k + 8 g + 4 h + r; as before
+// they are the second product's operand as they are.
+constexpr int TILE_WAVES = 8, TILE_ROWS = 32 * TILE_WAVES;
 template <int D, bool BF16, bool E4M3>
-__global__ __launch_bounds__(64 * TILE_WAVES) void tile_kernel(KvParams p) {
+__global__ __launch_bounds__(64 * TILE_WAVES, 2) void tile_kernel(KvParams p) {
   constexpr int BYTES = KV_BLOCK * D, PIECES = BYTES / 16, FRAGS = BYTES * 2 / 1024;
-  constexpr int PER = 2 * PIECES / (64 * TILE_WAVES);                 // 16-byte pieces of codes a thread converts
-  __shared__ uint4 lds[2][2][FRAGS * 64];                             // stage, keys / values
-  const int tid = threadIdx.x, l = tid & 63, i = l & 15, b4 = l >> 4;
+  constexpr int EACH = PIECES / (64 * TILE_WAVES);                    // pieces of keys, and of values, that a thread converts ...
+  constexpr int HELD = EACH ? 2 * EACH : 1;                           // (0: the first half of the threads keys, the others values)
+  __shared__ uint4 k_sh[2][FRAGS * 64], v_sh[2][FRAGS * 64];
+  const int tid = threadIdx.x, l = tid & 63, i = l & 31, half = l >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int H = p.kv_heads, G = p.q_heads / H;
   const int h = blockIdx.x % H, b = blockIdx.x / H % p.batch;
@@ -437,117 +543,143 @@ __global__ __launch_bounds__(64 * TILE_WAVES) void tile_kernel(KvParams p) {
   const int from = seen(p, place(r0), length).lo, upto = seen(p, place(r0 + TILE_ROWS - 1), length).hi;
   const int first = from / KV_BLOCK, end = upto > from ? (upto - 1) / KV_BLOCK + 1 : first;
   // the wavefront's own rows: seen by some of them, by all of them
-  const int w0 = r0 + wave * TILE_QT * 16;
-  const Seen seeA = seen(p, place(w0), length), seeZ = seen(p, place(w0 + TILE_QT * 16 - 1), length);
+  const int w0 = r0 + wave * 32, row = w0 + i;
+  const Seen seeA = seen(p, place(w0), length), seeZ = seen(p, place(w0 + 31), length);
   const int w_from = seeA.lo, w_upto = w0 < rows ? seeZ.hi : 0, lo = seeZ.lo, hi = seeA.hi;
 
-  half8 q[TILE_QT][D / 32];
-  float cs[TILE_QT];
-  Seen see[TILE_QT];
-  RowState st[TILE_QT];
-  float4v o[TILE_QT][D / 16];
+  const bool valid = row < rows;
+  Seen see = seen(p, s.before + row / G, length);
+  if (!valid) see.lo = see.hi = 0;
+  half8 q[D / 16];
+  const float cs = load_q_tall<D, BF16>(valid ? p.q + (int64_t)(s.first + row / G) * p.q_stride + (h * G + row % G) * D : nullptr, p.wide, half, q) * p.factor;
+  RowState st = {NONE, 0.0f};
+  float16v o[D / 32];
 #pragma unroll
-  for (int t = 0; t < TILE_QT; ++t) {
-    const int row = w0 + 16 * t + i;
-    const bool valid = row < rows;
-    see[t] = seen(p, s.before + row / G, length);
-    if (!valid) see[t].lo = see[t].hi = 0;
-    const uint16_t* q_row = valid ? p.q + (int64_t)(s.first + row / G) * p.q_stride + (h * G + row % G) * D : nullptr;
-    cs[t] = load_q<D, BF16>(q_row, p.wide, b4, q[t]) * p.factor;
-    st[t] = {NONE, 0.0f};
+  for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-    for (int d = 0; d < D / 16; ++d) o[t][d] = float4v{0, 0, 0, 0};
-  }
+    for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
 
   const int32_t* table = p.table + (int64_t)b * p.width;
-  uint4 raw[PER];
-  BlockScales bs = {0.0f, 0.0f, false};
-  const auto fetch = [&](int block) {
-    const uint32_t id = (uint32_t)table[block];
-    bs.there = id < (uint64_t)p.num_blocks;
-    const int64_t base = bs.there ? (int64_t)id * H + h : 0;
-    const float k = p.k_scale[base], v = p.v_scale[base];
-    bs.k = k; bs.v = v < SCALE_FLOOR ? SCALE_FLOOR : v;
+  struct Block : BlockScales { int64_t base; };
+  const auto find = [&](int block) {
+    Block x;
+    const uint32_t id = (uint32_t)table[min(block, end - 1)];
+    x.there = id < (uint64_t)p.num_blocks;
+    x.base = x.there ? (int64_t)id * H + h : 0;
+    x.k = p.k_scale[x.base]; x.v = p.v_scale[x.base];
+    return x;
+  };
+  uint4 raw[HELD];
+  const auto fetch = [&](const Block& x) {
+    const uint4* k = reinterpret_cast<const uint4*>(p.k_cache + x.base * BYTES);
+    const uint4* v = reinterpret_cast<const uint4*>(p.v_cache + x.base * BYTES);
+    if constexpr (EACH) {
 #pragma unroll
-    for (int n = 0; n < PER; ++n) {
-      const int piece = tid + n * 64 * TILE_WAVES;
-      raw[n] = reinterpret_cast<const uint4*>((piece < PIECES ? p.k_cache : p.v_cache) + base * BYTES)[piece % PIECES];
+      for (int n = 0; n < EACH; ++n) { raw[n] = k[tid + n * 64 * TILE_WAVES]; raw[EACH + n] = v[tid + n * 64 * TILE_WAVES]; }
+    } else {
+      raw[0] = tid < PIECES ? k[tid] : v[tid - PIECES];
     }
   };
-  const auto stage = [&](int block, int at) {
+  // Sixteen dimensions of a token: the two halves of operand (32 tokens, 16 dimensions), lanes of the token.
+  const auto put_k = [&](uint4* at, int piece, uint4 c) {
+    const int t = piece / D, ks = piece / 64 % (D / 64) * 4 + piece % 64 / 16;
+    uint4* to = at + ((t / 2 * (D / 16) + ks) * 64 + t % 2 * 16 + piece % 16);
+    to[0] = __builtin_bit_cast(uint4, numbers<E4M3>(c.x, c.y));
+    to[32] = __builtin_bit_cast(uint4, numbers<E4M3>(c.z, c.w));
+  };
+  // Sixteen tokens of a dimension, four of each of four operands (32 dimensions, 16 tokens).
+  const auto put_v = [&](uint4* at, int piece, uint4 c) {
+    const int f = piece / 64, b4 = piece % 64 / 16;
+    uint2* to = reinterpret_cast<uint2*>(at + (f / 2 * 4 * 64 + b4 % 2 * 32 + f % 2 * 16 + piece % 16)) + b4 / 2;
+    const uint4 lo4 = __builtin_bit_cast(uint4, numbers<E4M3>(c.x, c.y)), hi4 = __builtin_bit_cast(uint4, numbers<E4M3>(c.z, c.w));
+    to[0] = make_uint2(lo4.x, lo4.y); to[128] = make_uint2(lo4.z, lo4.w);
+    to[256] = make_uint2(hi4.x, hi4.y); to[384] = make_uint2(hi4.z, hi4.w);
+  };
+  // bytes of tokens that are not there may be anything, also NaN
+  const auto only_there = [&](uint4 c, int piece, int block, bool there) {
+    if (E4M3 && (!there || block * KV_BLOCK + KV_BLOCK > length)) {
+      const int token0 = block * KV_BLOCK + 4 * (piece % 64 / 16), n = there ? length : 0;
+      c.x &= bytes_below(n - token0); c.y &= bytes_below(n - token0 - 16);
+      c.z &= bytes_below(n - token0 - 32); c.w &= bytes_below(n - token0 - 48);
+    }
+    return c;
+  };
+  const auto stage = [&](int block, bool there) {
+    const int at = block & 1;
+    if constexpr (EACH) {
 #pragma unroll
-    for (int n = 0; n < PER; ++n) {
-      const int piece = (tid + n * 64 * TILE_WAVES) % PIECES, which = (tid + n * 64 * TILE_WAVES) / PIECES;
-      uint4 c = raw[n];
-      if (E4M3 && which == 1 && (!bs.there || block * KV_BLOCK + KV_BLOCK > length)) {
-        const int token0 = block * KV_BLOCK + 4 * (piece % 64 / 16), upto = bs.there ? length : 0;
-        c.x &= bytes_below(upto - token0); c.y &= bytes_below(upto - token0 - 16);
-        c.z &= bytes_below(upto - token0 - 32); c.w &= bytes_below(upto - token0 - 48);
+      for (int n = 0; n < EACH; ++n) {
+        const int piece = tid + n * 64 * TILE_WAVES;
+        put_k(k_sh[at], piece, raw[n]);
+        put_v(v_sh[at], piece, only_there(raw[EACH + n], piece, block, there));
       }
-      uint4* to = &lds[at][which][piece / 64 * 128 + piece % 64];
-      to[0] = __builtin_bit_cast(uint4, numbers<E4M3>(c.x, c.y));
-      to[64] = __builtin_bit_cast(uint4, numbers<E4M3>(c.z, c.w));
+    } else {
+      if (tid < PIECES) put_k(k_sh[at], tid, raw[0]);
+      else              put_v(v_sh[at], tid - PIECES, only_there(raw[0], tid - PIECES, block, there));
     }
   };
-  BlockScales now = bs;
-  if (first < end) { fetch(first); stage(first, 0); now = bs; }
-  __syncthreads();
-  for (int block = first, at = 0; block < end; ++block, at ^= 1) {
-    if (block + 1 < end) fetch(block + 1);
-    const int t0 = block * KV_BLOCK;
-    if (t0 < w_upto && t0 + KV_BLOCK > w_from) {
-      const uint4* kf = &lds[at][0][l];
-      const uint4* vf = &lds[at][1][l];
-      float4v acc[TILE_QT][4];
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-#pragma unroll
-        for (int n = 0; n < TILE_QT; ++n) acc[n][t] = float4v{0, 0, 0, 0};
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          const half8 a = __builtin_bit_cast(half8, kf[(t * (D / 32) + c) * 64]);
-#pragma unroll
-          for (int n = 0; n < TILE_QT; ++n) acc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, q[n][c], acc[n][t], 0, 0, 0);
-        }
-      }
-      const float lv = __builtin_amdgcn_logf(now.v), ivs = 1.0f / now.v;
-      const bool edge = !now.there || t0 < lo || t0 + KV_BLOCK > hi;
-      half8 P[TILE_QT][2];
-      float alpha[TILE_QT];
-#pragma unroll
-      for (int n = 0; n < TILE_QT; ++n) {
-        if (edge) alpha[n] = softmax_step<true>(acc[n], P[n], st[n], cs[n] * now.k, lv, ivs, t0 + 4 * b4, now.there ? see[n] : Seen{0, 0});
-        else      alpha[n] = softmax_step<false>(acc[n], P[n], st[n], cs[n] * now.k, lv, ivs, t0 + 4 * b4, see[n]);
-      }
-#pragma unroll
-      for (int n = 0; n < TILE_QT; ++n)
-        if (__ballot(alpha[n] != 1.0f)) {
-#pragma unroll
-          for (int d = 0; d < D / 16; ++d) o[n][d] *= alpha[n];
-        }
-#pragma unroll
-      for (int d = 0; d < D / 16; ++d)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const half8 a = __builtin_bit_cast(half8, vf[(2 * d + k) * 64]);
-#pragma unroll
-          for (int n = 0; n < TILE_QT; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, P[n][k], o[n][d], 0, 0, 0);
-        }
-    }
-    if (block + 1 < end) { stage(block + 1, at ^ 1); now = bs; }
+
+  if (first < end) {
+    Block now = find(first);
+    fetch(now);
+    stage(first, now.there);
     __syncthreads();
-  }
+    for (int block = first; block < end; ++block) {
+      const Block next = find(block + 1);
+      fetch(next);
+      const int t0 = block * KV_BLOCK;
+      if (t0 < w_upto && t0 + KV_BLOCK > w_from) {
+        const uint4* kf = &k_sh[block & 1][l];
+        const uint4* vf = &v_sh[block & 1][l];
+        // operands are read from LDS a group ahead of the matrix instructions that take them: two steps of 16 dimensions,
+        // two tiles of 32 tokens; then a step of 16 tokens, all dimensions
+        half8 a[2][4];
+        const auto read_k = [&](int g) {
 #pragma unroll
-  for (int n = 0; n < TILE_QT; ++n) {
-    const int row = w0 + 16 * n + i;
-    const float L = column_sum(st[n].l);
-    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-    if (row >= rows) continue;
-    uint16_t* out = p.out + ((int64_t)(s.first + row / G) * p.q_heads + h * G + row % G) * D + 4 * b4;
+          for (int c = 0; c < 4; ++c) a[g & 1][c] = __builtin_bit_cast(half8, kf[(c % 2 * (D / 16) + 2 * g + c / 2) * 64]);
+        };
+        const auto read_v = [&](int g) {
 #pragma unroll
-    for (int d = 0; d < D / 16; ++d)
-      *reinterpret_cast<uint2*>(out + 16 * d) = make_uint2(pack2<BF16>(o[n][d][0] * inv, o[n][d][1] * inv), pack2<BF16>(o[n][d][2] * inv, o[n][d][3] * inv));
+          for (int d = 0; d < D / 32; ++d) a[g & 1][d] = __builtin_bit_cast(half8, vf[(d * 4 + g) * 64]);
+        };
+        float16v acc[2];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[0][r] = acc[1][r] = 0.0f;
+        read_k(0);
+#pragma unroll
+        for (int g = 0; g < D / 32; ++g) {
+          if (g + 1 < D / 32) read_k(g + 1);
+          else                read_v(0);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[c % 2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[g & 1][c], q[2 * g + c / 2], acc[c % 2], 0, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        half8 P[4];
+        tall_softmax_step(acc, P, o, st, cs, see, now, !now.there || t0 < lo || t0 + KV_BLOCK > hi, t0 + 4 * half);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          if (g + 1 < 4) read_v(g + 1);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int d = 0; d < D / 32; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[g & 1][d], P[g], o[d], 0, 0, 0);
+        }
+      }
+      stage(block + 1, next.there);
+      now = next;
+      __syncthreads();
+    }
   }
+  const float L = half_sum(st.l);
+  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+  if (!valid) return;
+  uint16_t* out = p.out + ((int64_t)(s.first + row / G) * p.q_heads + h * G + row % G) * D + 4 * half;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<uint2*>(out + 32 * d + 8 * g) =
+          make_uint2(pack2<BF16>(o[d][4 * g] * inv, o[d][4 * g + 1] * inv), pack2<BF16>(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv));
 }
 
 // How long a part is.  Workgroups read at some 40 GB/s each, so as many as there are CUs stream the cache at its rate, and more
