@@ -19,7 +19,7 @@
 extern "C" {
 #endif
 
-/* Sets override `knob` (0..3) to `value` (0 = automatic) and returns the previous value.
+/* Sets override `knob` (0..5) to `value` (0 = automatic) and returns the previous value.
  *   knob 0: forced path (1 = streaming kernel, M <= 64 only; 2 = tiled kernel; 3 = streaming
  *           kernel over blocks of 64 rows; 4 = the paper's prefill variant, Section "End-to-End
  *           Performance": the whole weight is de-quantised to 16 bits first, into a
@@ -42,7 +42,10 @@ extern "C" {
  *           16 on 4.  Several: 21, 31, 41 are 8 wavefronts on one strip, 26, 36, 46 are 8 on 2; 22, 32, 42
  *           are 4 on one strip, 27, 37, 47 4 on 2.  Group 32 with 16-bit scales takes no forced one.  Its row tiles
  *           must be the ones M needs (1 up to 16 rows, 2 up to 32, 3 up to 48, 4 from 33 to 64), else QG_EINVAL.
- * Knobs 0, 1 and 3 apply to QG_LAYOUT_TILE128x64 only. */
+ * Knobs 0, 1 and 3 apply to QG_LAYOUT_TILE128x64 only.
+ *   knob 4: forced kernel of qg_kv_attention (1 = streaming kernel, 2 / 3 = tiled kernel with 128 / 256 rows; 3 has heads of 128
+ *           only, else QG_EINVAL)
+ *   knob 5: blocks of the cache to a part of qg_kv_attention, where there is a workspace for the parts */
 QG_API int qg_set_knob(int knob, int value);
 
 #ifdef __cplusplus

@@ -31,6 +31,7 @@ int launch_clear(void*, size_t, hipStream_t);
 size_t layer_workspace_bytes();
 int layer_workspace(size_t, size_t, hipStream_t, float**, unsigned**);
 void layer_error(const char*);
+int layer_knob(int);
 // codebook indices of 1..8 bits: kernel-side weight types WT_LUT0 .. WT_LUT0 + 7
 #define QG_FOR_ALL_LUT(X) X(15) X(16) X(17) X(18) X(19) X(20) X(21) X(22)
 #define QG_DECL(i)                                                            \
@@ -85,8 +86,9 @@ static const waves_fn kDecodeWaves[NUM_WT] = {QG_FOR_ALL_WT(QG_ENT)};
 
 static thread_local std::string g_last_error;
 // Experiment overrides (qg_set_knob): process-wide, read once per call with relaxed loads.
-static std::atomic<int> g_knob[4] = {{0}, {0}, {0}, {0}};
+static std::atomic<int> g_knob[6] = {{0}, {0}, {0}, {0}, {0}, {0}};
 static int knob(int i) { return g_knob[i].load(std::memory_order_relaxed); }
+int layer_knob(int i) { return knob(i); }
 
 // A failed call's error is reported by the status, so it is read away here: the runtime keeps it until
 // hipGetLastError, and the check behind the next launch would take it for that launch's.
@@ -1121,7 +1123,7 @@ int qg_plan(qg_wtype t, int layout, int act, int scale_dtype, int64_t group, int
 }
 
 int qg_set_knob(int knob, int value) {
-  if (knob < 0 || knob >= 4) return 0;
+  if (knob < 0 || knob >= 6) return 0;
   return g_knob[knob].exchange(value, std::memory_order_relaxed);
 }
 

@@ -161,20 +161,16 @@ __device__ __forceinline__ float top_score(const float4v (&acc)[4]) {
   for (int t = 1; t < 4; ++t) top = top_of(top, top_of(top_of(acc[t][0], acc[t][1]), top_of(acc[t][2], acc[t][3])));
   return top;
 }
-// The reference, from each lane's largest product: moved where one of a column's four lanes is MOVE_BY above it.  Returns
-// whether any is; then the accumulators have to be multiplied by alpha.
-template <class Column>
-__device__ __forceinline__ bool move_reference(float top, RowState& st, float f, float lv, float& alpha, Column column) {
+// The reference, from the row's largest product in the block.  Returns the factor for what was summed before (1: none).
+__device__ __forceinline__ float move_reference(float top, RowState& st, float f, float lv) {
   top = fmaf(top, f, lv);                                    // NaN (a scale, a score) does not move it: the row is NaN
-  if (!__ballot(top > st.m + MOVE_BY)) return false;
-  top = column(top);
-  alpha = 1.0f;
+  float alpha = 1.0f;
   if (top > st.m + MOVE_BY) {
     alpha = st.m == NONE ? 0.0f : __builtin_amdgcn_exp2f(st.m - top);
     st.m = top;
     st.l *= alpha;
   }
-  return true;
+  return alpha;
 }
 
 // Four tokens' scores to P', c = lv - reference; returns their sum.
@@ -200,41 +196,20 @@ __device__ __forceinline__ void probabilities(const float4v (&acc)[4], half8 (&P
   for (int t = 0; t < 4; ++t) sum += four_probabilities<EDGE>(acc[t], P[t / 2], 4 * (t % 2), f, c, token0 + 16 * t, see);
   add_sum(st, sum, ivs);
 }
+// All of it for one tile; returns the factor that its accumulators have to be multiplied by.  (Here the maximum goes over the
+// column on every block: what a branch would save costs more in registers, and this kernel waits for memory.)
+template <bool EDGE>
+__device__ __forceinline__ float softmax_step(float4v (&acc)[4], half8 (&P)[2], RowState& st, float f, float lv, float ivs, int token0, Seen see) {
+  if constexpr (EDGE) mask_scores(acc, token0, see);
+  const float alpha = move_reference(column_max(top_score(acc)), st, f, lv);
+  probabilities<EDGE>(acc, P, st, f, lv, ivs, token0, see);
+  return alpha;
+}
+
 // The same number, unknown to the compiler: what is computed from it stays in the branch that asks for it.
 __device__ __forceinline__ int hidden(int x) {
   asm volatile("" : "+v"(x));
   return x;
-}
-// All of it, for T tiles and their accumulators o.  edge: some row does not see some token.
-template <int T, int N>
-__device__ __forceinline__ void softmax_step(float4v (&acc)[T][4], half8 (&P)[T][2], float4v (&o)[T][N], RowState (&st)[T], const float (&cs)[T],
-                                             const Seen (&see)[T], const BlockScales& block, bool edge, int token0) {
-  const float vs = block.v < SCALE_FLOOR ? SCALE_FLOOR : block.v;
-  const float lv = __builtin_amdgcn_logf(vs), ivs = 1.0f / vs;
-  Seen my[T];
-#pragma unroll
-  for (int n = 0; n < T; ++n) my[n] = block.there ? see[n] : Seen{0, 0};
-  if (edge) {
-    const int token = hidden(token0);
-#pragma unroll
-    for (int n = 0; n < T; ++n) mask_scores(acc[n], token, my[n]);
-  }
-#pragma unroll
-  for (int n = 0; n < T; ++n) {
-    float alpha;
-    if (move_reference(top_score(acc[n]), st[n], cs[n] * block.k, lv, alpha, column_max)) {
-#pragma unroll
-      for (int d = 0; d < N; ++d) o[n][d] *= alpha;
-    }
-  }
-  if (edge) {
-    const int token = hidden(token0);
-#pragma unroll
-    for (int n = 0; n < T; ++n) probabilities<true>(acc[n], P[n], st[n], cs[n] * block.k, lv, ivs, token, my[n]);
-  } else {
-#pragma unroll
-    for (int n = 0; n < T; ++n) probabilities<false>(acc[n], P[n], st[n], cs[n] * block.k, lv, ivs, token0, my[n]);
-  }
 }
 
 // The same for the 32 scores that a lane has with the 32x32x16 instruction: register r of tile k is token
@@ -262,7 +237,7 @@ template <int N>
 __device__ __forceinline__ void tall_softmax_step(float16v (&acc)[2], half8 (&P)[4], float16v (&o)[N], RowState& st, float cs, Seen see,
                                                   const BlockScales& block, bool edge, int token0) {
   const float vs = block.v < SCALE_FLOOR ? SCALE_FLOOR : block.v;
-  const float lv = __builtin_amdgcn_logf(vs), ivs = 1.0f / vs, f = cs * block.k;
+  const float lv = __builtin_amdgcn_logf(vs), ivs = __builtin_amdgcn_rcpf(vs), f = cs * block.k;
   const Seen my = block.there ? see : Seen{0, 0};
   if (edge) {
     const int token1 = hidden(token0);
@@ -277,8 +252,8 @@ __device__ __forceinline__ void tall_softmax_step(float16v (&acc)[2], half8 (&P)
   float top = top_of(acc[0][0], acc[1][0]);
 #pragma unroll
   for (int r = 1; r < 16; ++r) top = top_of(top, top_of(acc[0][r], acc[1][r]));
-  float alpha;
-  if (move_reference(top, st, f, lv, alpha, half_max)) {
+  if (__ballot(fmaf(top, f, lv) > st.m + MOVE_BY)) {          // either lane of a row
+    const float alpha = move_reference(half_max(top), st, f, lv);
 #pragma unroll
     for (int d = 0; d < N; ++d) o[d] *= alpha;
   }
@@ -392,17 +367,31 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, 2) void stream_kernel(KvParams p
       next_id = (uint32_t)table[min(next + STREAM_WAVES, end - 1)];
       load_k();
     }
+    const float vs = now.v < SCALE_FLOOR ? SCALE_FLOOR : now.v;
+    const float lv = __builtin_amdgcn_logf(vs), ivs = __builtin_amdgcn_rcpf(vs);
     const int token0 = block * KV_BLOCK + 4 * b4;
-    const bool edge = !now.there || block * KV_BLOCK < lo || block * KV_BLOCK + KV_BLOCK > hi;
     half8 P[T][2];
-    softmax_step<T>(acc, P, o, st, cs, see, now, edge, token0);
-    if (E4M3 && edge) {      // bytes of tokens that are not there may be anything, also NaN
-      uint32_t keep[4];
+    float alpha[T];
+    if (!now.there || block * KV_BLOCK < lo || block * KV_BLOCK + KV_BLOCK > hi) {       // some row does not see some token
 #pragma unroll
-      for (int t = 0; t < 4; ++t) keep[t] = now.there ? bytes_below(length - (token0 + 16 * t)) : 0u;
+      for (int n = 0; n < T; ++n) alpha[n] = softmax_step<true>(acc[n], P[n], st[n], cs[n] * now.k, lv, ivs, token0, now.there ? see[n] : Seen{0, 0});
+      if constexpr (E4M3) {      // bytes of tokens that are not there may be anything, also NaN
+        uint32_t keep[4];
 #pragma unroll
-      for (int j = 0; j < LOADS; ++j) { V[j].x &= keep[0]; V[j].y &= keep[1]; V[j].z &= keep[2]; V[j].w &= keep[3]; }
+        for (int t = 0; t < 4; ++t) keep[t] = now.there ? bytes_below(length - (token0 + 16 * t)) : 0u;
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) { V[j].x &= keep[0]; V[j].y &= keep[1]; V[j].z &= keep[2]; V[j].w &= keep[3]; }
+      }
+    } else {
+#pragma unroll
+      for (int n = 0; n < T; ++n) alpha[n] = softmax_step<false>(acc[n], P[n], st[n], cs[n] * now.k, lv, ivs, token0, see[n]);
     }
+#pragma unroll
+    for (int n = 0; n < T; ++n)
+      if (__ballot(alpha[n] != 1.0f)) {
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) o[n][d] *= alpha[n];
+      }
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -455,7 +444,7 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, 2) void stream_kernel(KvParams p
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    unsigned* ticket = p.tickets + (int64_t)blockIdx.x * p.tiles;            // p.tiles: distance of counters
+    unsigned* ticket = p.tickets + (int64_t)blockIdx.x * p.stride;
     if (tid == 0) last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)(parts - 1);
     __syncthreads();
     if (!last) return;
@@ -523,25 +512,33 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, 2) void stream_kernel(KvParams p
 // matrix instruction is the 32x32x16 one: half as many of them issue, and a lane holds 32 scores of one row, so that there
 // is one reference and one sum to a lane.  Lane 32 h + i gets the scores of row i and tokens 32 k + 8 g + 4 h + r; as before
 // they are the second product's operand as they are.
-constexpr int TILE_WAVES = 8, TILE_ROWS = 32 * TILE_WAVES;
-template <int D, bool BF16, bool E4M3>
-__global__ __launch_bounds__(64 * TILE_WAVES, 2) void tile_kernel(KvParams p) {
+// Partial results of one wavefront and part: accumulators, reference and sum of every lane.
+template <int D>
+constexpr int TILE_PART = 64 * (D / 2 + 2);
+template <int D, bool BF16, bool E4M3, int W>
+__global__ __launch_bounds__(64 * W, 2) void tile_kernel(KvParams p) {
+  constexpr int TILE_ROWS = 32 * W;
   constexpr int BYTES = KV_BLOCK * D, PIECES = BYTES / 16, FRAGS = BYTES * 2 / 1024;
-  constexpr int EACH = PIECES / (64 * TILE_WAVES);                    // pieces of keys, and of values, that a thread converts ...
+  constexpr int EACH = PIECES / (64 * W);                    // pieces of keys, and of values, that a thread converts ...
   constexpr int HELD = EACH ? 2 * EACH : 1;                           // (0: the first half of the threads keys, the others values)
   __shared__ uint4 k_sh[2][FRAGS * 64], v_sh[2][FRAGS * 64];
   const int tid = threadIdx.x, l = tid & 63, i = l & 31, half = l >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int H = p.kv_heads, G = p.q_heads / H;
   const int h = blockIdx.x % H, b = blockIdx.x / H % p.batch;
-  const int tile = p.tiles - 1 - (int)(blockIdx.x / H / p.batch);      // rows that see most start first
+  const int tile = (int)(gridDim.x / H / p.batch) - 1 - (int)(blockIdx.x / H / p.batch);      // rows that see most start first
   const Sequence s = sequence(p, b);
   const int rows = s.rows * G, r0 = tile * TILE_ROWS;
   if (r0 >= rows) return;
   const int length = (int)min((int64_t)max(s.length, 0), p.width * KV_BLOCK);
   const auto place = [&](int row) { return s.before + min(row, rows - 1) / G; };
   const int from = seen(p, place(r0), length).lo, upto = seen(p, place(r0 + TILE_ROWS - 1), length).hi;
-  const int first = from / KV_BLOCK, end = upto > from ? (upto - 1) / KV_BLOCK + 1 : first;
+  const int all = upto > from ? (upto - 1) / KV_BLOCK + 1 - from / KV_BLOCK : 0;
+  // p.splits: blocks to a part, as in the streaming kernel
+  const int each = max(p.splits, (int)((all + gridDim.y - 1) / gridDim.y));
+  const int parts = max((all + each - 1) / each, 1), part = blockIdx.y;
+  if (part >= parts) return;
+  const int first = from / KV_BLOCK + part * each, end = min(first + each, from / KV_BLOCK + all);
   // the wavefront's own rows: seen by some of them, by all of them
   const int w0 = r0 + wave * 32, row = w0 + i;
   const Seen seeA = seen(p, place(w0), length), seeZ = seen(p, place(w0 + 31), length);
@@ -575,7 +572,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 2) void tile_kernel(KvParams p) {
     const uint4* v = reinterpret_cast<const uint4*>(p.v_cache + x.base * BYTES);
     if constexpr (EACH) {
 #pragma unroll
-      for (int n = 0; n < EACH; ++n) { raw[n] = k[tid + n * 64 * TILE_WAVES]; raw[EACH + n] = v[tid + n * 64 * TILE_WAVES]; }
+      for (int n = 0; n < EACH; ++n) { raw[n] = k[tid + n * 64 * W]; raw[EACH + n] = v[tid + n * 64 * W]; }
     } else {
       raw[0] = tid < PIECES ? k[tid] : v[tid - PIECES];
     }
@@ -609,7 +606,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 2) void tile_kernel(KvParams p) {
     if constexpr (EACH) {
 #pragma unroll
       for (int n = 0; n < EACH; ++n) {
-        const int piece = tid + n * 64 * TILE_WAVES;
+        const int piece = tid + n * 64 * W;
         put_k(k_sh[at], piece, raw[n]);
         put_v(v_sh[at], piece, only_there(raw[EACH + n], piece, block, there));
       }
@@ -670,7 +667,47 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 2) void tile_kernel(KvParams p) {
       __syncthreads();
     }
   }
-  const float L = half_sum(st.l);
+  float L = half_sum(st.l);
+  if (parts > 1) {
+    // A wavefront's parts meet by themselves, in the order of the tokens: accumulators lie in the workspace as in the lanes.
+    if (w0 >= rows) return;
+    constexpr int SIZE = TILE_PART<D>, PAIRS = D / 4;
+    float* const mine = p.partial + (((int64_t)blockIdx.x * gridDim.y) * W + wave) * SIZE;
+    const auto slot = [&](int k, int pair) { return reinterpret_cast<unsigned long long*>(mine + (int64_t)k * W * SIZE) + pair * 64 + l; };
+    const auto two = [](float x, float y) { return __builtin_bit_cast(uint32_t, x) | (unsigned long long)__builtin_bit_cast(uint32_t, y) << 32; };
+    const auto lower = [](unsigned long long u) { return __builtin_bit_cast(float, (uint32_t)u); };
+    const auto upper = [](unsigned long long u) { return __builtin_bit_cast(float, (uint32_t)(u >> 32)); };
+#pragma unroll
+    for (int n = 0; n < PAIRS; ++n)
+      __hip_atomic_store(slot(part, n), two(o[n / 8][n % 8 * 2], o[n / 8][n % 8 * 2 + 1]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(slot(part, PAIRS), two(st.m, L), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    unsigned* ticket = p.tickets + ((int64_t)blockIdx.x * W + wave) * p.stride;
+    unsigned came = 0;
+    if (l == 0) came = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (__builtin_amdgcn_readfirstlane(came) != (unsigned)(parts - 1)) return;
+    if (l == 0) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    float M = NONE;
+    for (int k = 0; k < parts; ++k) M = fmaxf(M, lower(__hip_atomic_load(slot(k, PAIRS), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)));
+    L = 0.0f;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
+    for (int k = 0; k < parts; ++k) {
+      unsigned long long u[PAIRS];
+      const unsigned long long ml = __hip_atomic_load(slot(k, PAIRS), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+      for (int n = 0; n < PAIRS; ++n) u[n] = __hip_atomic_load(slot(k, n), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      const float f = M == NONE ? 1.0f : __builtin_amdgcn_exp2f(lower(ml) - M);
+      L = fmaf(f, upper(ml), L);
+#pragma unroll
+      for (int n = 0; n < PAIRS; ++n) {
+        o[n / 8][n % 8 * 2] = fmaf(f, lower(u[n]), o[n / 8][n % 8 * 2]);
+        o[n / 8][n % 8 * 2 + 1] = fmaf(f, upper(u[n]), o[n / 8][n % 8 * 2 + 1]);
+      }
+    }
+  }
   const float inv = L == 0.0f ? 0.0f : 1.0f / L;
   if (!valid) return;
   uint16_t* out = p.out + ((int64_t)(s.first + row / G) * p.q_heads + h * G + row % G) * D + 4 * half;
@@ -682,46 +719,76 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 2) void tile_kernel(KvParams p) {
           make_uint2(pack2<BF16>(o[d][4 * g] * inv, o[d][4 * g + 1] * inv), pack2<BF16>(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv));
 }
 
-// How long a part is.  Workgroups read at some 40 GB/s each, so as many as there are CUs stream the cache at its rate, and more
-// only add partial results; parts of less than four blocks do not pay for their meeting, and parts of at most 128 keep one
-// long sequence among short ones from being the last one left.  One row tile, 64 heads over 8, us:
-//   1 x 131071 tokens (8 units): 32 / 64 / 128 blocks 55 / 48 / 53;    64 x 1000 .. 8000 (512 units): 108.. for 128, 114 for 64, 119 for 32
+// The grid's second dimension: parts of `chunk` blocks, in a workspace for `units` tiles of `waves` partial results of `floats`
+// each.  Without a workspace one part.
+static unsigned cut(KvParams& p, int64_t units, int64_t blocks, int64_t chunk, int waves, int floats, hipStream_t st) {
+  const size_t bytes = (size_t)units * waves * floats * sizeof(float);
+  const int64_t counters = units * waves;
+  int64_t parts = 1;
+  if (layer_knob(5) > 0) chunk = layer_knob(5);
+  if (chunk < blocks && bytes < layer_workspace_bytes() && counters <= WS_TICKETS) {
+    const int64_t most = std::min<int64_t>(layer_workspace_bytes() / bytes, 65535);
+    chunk = std::max(chunk, (blocks + most - 1) / most);
+    parts = (blocks + chunk - 1) / chunk;
+    p.stride = ticket_stride(counters);
+    if (parts > 1 && layer_workspace(bytes * parts, (size_t)(counters * p.stride), st, &p.partial, &p.tickets) != QG_OK) parts = 1;
+  }
+  p.splits = (int)std::min<int64_t>(parts == 1 ? blocks : chunk, INT32_MAX / KV_BLOCK);
+  return (unsigned)parts;
+}
+
+// Streaming, how long a part is.  Workgroups read at some 40 GB/s each, so as many as there are CUs stream the cache at its rate, and
+// more only add partial results; parts of less than four blocks do not pay for their meeting, and parts of at most 128 keep
+// one long sequence among short ones from being the last one left.  One row tile, 64 heads over 8, us:
+//   1 x 131071 tokens (8 units): 32 / 64 / 128 blocks 55 / 48 / 53;    64 x 1000 .. 8000 (512 units): 119 / 114 / 108
 //   8 x 500 .. 4000 (64 units):  8 / 16 / 32 blocks 17 / 13 / 17;      1 x 1000 (8 units): 4 / 8 / 16 blocks 7.6 / 8.8 / 8.8
 template <int D, bool BF16, bool E4M3, int T>
-static int launch_stream(KvParams& p, int64_t max_tile_rows, int64_t max_kv, hipStream_t st) {
+static int launch_stream(KvParams& p, int64_t max_tile_rows, int64_t blocks, hipStream_t st) {
   const int64_t tiles = (max_tile_rows + 16 * T - 1) / (16 * T), units = tiles * p.kv_heads * p.batch;
   if (units > MOST_GROUPS) return QG_EUNSUPPORTED;
-  const int64_t blocks = std::max<int64_t>((max_kv + KV_BLOCK - 1) / KV_BLOCK, 1);
-  const size_t part = PART<D, T> * sizeof(float);
-  int64_t chunk = std::clamp<int64_t>((units * blocks + 255) / 256, 4, 128);
-  while (chunk < blocks && (size_t)units * ((blocks + chunk - 1) / chunk) * part > layer_workspace_bytes()) chunk *= 2;
-  int64_t parts = (blocks + chunk - 1) / chunk;
-  p.tiles = ticket_stride(units);
-  if (parts > 1 && (parts > 65535 || p.tiles * units > WS_TICKETS ||
-                    layer_workspace((size_t)units * parts * part, (size_t)(units * p.tiles), st, &p.partial, &p.tickets) != QG_OK)) {
-    parts = 1;
-    chunk = blocks;
-  }
-  p.splits = (int)std::min<int64_t>(chunk, INT32_MAX / KV_BLOCK);
-  const dim3 grid((unsigned)units, (unsigned)parts), threads(64 * STREAM_WAVES);
+  const unsigned parts = cut(p, units, blocks, std::clamp<int64_t>((units * blocks + 255) / 256, 4, 128), 1, PART<D, T>, st);
+  const dim3 grid((unsigned)units, parts), threads(64 * STREAM_WAVES);
   if (tiles > 1) hipLaunchKernelGGL((stream_kernel<D, BF16, E4M3, T, true>), grid, threads, 0, st, p);
   else           hipLaunchKernelGGL((stream_kernel<D, BF16, E4M3, T, false>), grid, threads, 0, st, p);
   return hipGetLastError() == hipSuccess ? QG_OK : QG_EHIP;
 }
 
+// Tiles: parts where there are fewer tiles than the GPU holds at once, of at least eight blocks (800 rows on 4000 tokens: 40 us, uncut 103).
+template <int D, bool BF16, bool E4M3, int W>
+static int launch_tiles(KvParams& p, int64_t max_tile_rows, int64_t blocks, hipStream_t st) {
+  const int64_t tiles = (max_tile_rows + 32 * W - 1) / (32 * W), units = tiles * p.kv_heads * p.batch;
+  if (units > MOST_GROUPS) return QG_EUNSUPPORTED;
+  constexpr int AT_ONCE = 256 * (D == 64 ? 3 : 8 / W);       // workgroups that the GPU holds
+  const unsigned parts = cut(p, units, blocks, std::max<int64_t>((units * blocks + AT_ONCE - 1) / AT_ONCE, 8), W, TILE_PART<D>, st);
+  hipLaunchKernelGGL((tile_kernel<D, BF16, E4M3, W>), dim3((unsigned)units, parts), dim3(64 * W), 0, st, p);
+  return hipGetLastError() == hipSuccess ? QG_OK : QG_EHIP;
+}
+
+// Which kernel.  The streaming one converts a block for every 32 rows anew and reads it again through the caches, but needs no
+// workgroup to wait for its neighbours: 600 TFLOP/s at most, but with few rows it is there sooner.  us, streaming / tiled, 32 query
+// heads over 8, 128 wide:
+//   192 rows of 8 sequences, 4000 tokens 38 / 54    400 rows of 4, 2000 tokens 35 / 39    800 rows of one, 4000 tokens 39 / 40
+//   1600 rows of one, 4000 tokens 58 / 54           800 rows of 4, 2000 tokens 68 / 50    800 rows of one, 30000 tokens 177 / 141
+// So it takes up to 192 rows of a sequence and head, and more while all rows make two rounds of 256 workgroups that have some
+// 40 blocks each.
+// Tiles of 256 rows (128 wide heads) where they fill the GPU twice: 1080 us against 1145 of 128-row tiles for 8192 tokens, 64 heads over
+// 8; below, 128-row tiles leave fewer CUs without one (512 tokens on 8000: 198 against 240).  64 wide heads have registers for three
+// wavefronts on a SIMD, and workgroups of four to use them (8192 tokens, 40 heads over 8: 419 against 500).
 template <int D, bool BF16, bool E4M3>
 static int launch_attention(KvParams& p, int64_t max_kv, hipStream_t st) {
-  const int G = p.q_heads / p.kv_heads;
-  const int64_t max_tile_rows = (int64_t)p.max_rows * G;
-  if (max_tile_rows > 64) {
-    const int64_t tiles = (max_tile_rows + TILE_ROWS - 1) / TILE_ROWS, grid = tiles * p.kv_heads * p.batch;
-    if (grid > MOST_GROUPS) return QG_EUNSUPPORTED;
-    p.tiles = (int)tiles;
-    hipLaunchKernelGGL((tile_kernel<D, BF16, E4M3>), dim3((unsigned)grid), dim3(64 * TILE_WAVES), 0, st, p);
-    return hipGetLastError() == hipSuccess ? QG_OK : QG_EHIP;
-  }
-  return max_tile_rows <= 16 ? launch_stream<D, BF16, E4M3, 1>(p, max_tile_rows, max_kv, st)
-                             : launch_stream<D, BF16, E4M3, 2>(p, max_tile_rows, max_kv, st);
+  const int64_t rows = (int64_t)p.max_rows * (p.q_heads / p.kv_heads);      // of one sequence and key/value head, at most
+  const int64_t blocks = std::max<int64_t>((max_kv + KV_BLOCK - 1) / KV_BLOCK, 1), heads = (int64_t)p.kv_heads * p.batch;
+  const int forced = layer_knob(4);
+  if (forced < 0 || forced > 3 || (forced == 3 && D != 128)) return QG_EINVAL;
+  if (forced == 2) return launch_tiles<D, BF16, E4M3, 4>(p, rows, blocks, st);
+  if constexpr (D == 128)
+    if (forced == 3) return launch_tiles<D, BF16, E4M3, 8>(p, rows, blocks, st);
+  if (rows <= 16) return launch_stream<D, BF16, E4M3, 1>(p, rows, blocks, st);
+  const int64_t groups = (rows + 31) / 32 * heads;
+  if (forced == 1 || rows <= 192 || (groups <= 512 && groups * blocks <= 20000)) return launch_stream<D, BF16, E4M3, 2>(p, rows, blocks, st);
+  if constexpr (D == 128)
+    if ((rows + 255) / 256 * heads >= 512) return launch_tiles<D, BF16, E4M3, 8>(p, rows, blocks, st);
+  return launch_tiles<D, BF16, E4M3, 4>(p, rows, blocks, st);
 }
 
 int kv_attention_launch(KvParams& p, int head_dim, int64_t max_kv, hipStream_t st) {

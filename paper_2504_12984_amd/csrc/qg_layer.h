@@ -117,7 +117,8 @@ struct KvParams {
   float factor;                        // scale * log2(e)
   int causal;
   int window;                          // 0: none
-  int splits, tiles;
+  int splits;                          // blocks to a part
+  int stride;                          // of the arrival counters
   float* partial; unsigned* tickets;
 };
 
@@ -147,5 +148,6 @@ int kv_attention_launch(KvParams&, int head_dim, int64_t max_kv, hipStream_t);
 int layer_workspace(size_t partial_bytes, size_t counters, hipStream_t, float** partial, unsigned** tickets);
 size_t layer_workspace_bytes();
 void layer_error(const char* text);
+int layer_knob(int i);                 // experiment overrides, see include/qgemm_tuning.h
 
 }  // namespace qg

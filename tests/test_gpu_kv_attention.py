@@ -71,6 +71,112 @@ def test_attention(case):
     check(S, q, out, act, causal, window, D ** -0.5)
 
 
+@pytest.fixture
+def forced():
+    from paper_2504_12984_amd import binding as B
+
+    def force(kernel, blocks=0):
+        B.qg_set_knob(4, kernel)
+        B.qg_set_knob(5, blocks)
+    yield force
+    force(0)
+
+
+KERNELS = [1, 2, 3]          # streaming, 128-row tiles, 256-row tiles
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("case", CASES, ids=[str(i) for i in range(len(CASES))])
+def test_attention_by_each_kernel(case, kernel, forced):
+    from paper_2504_12984_amd import binding as B
+    new, length, H, Hq, D, kv, act, causal, window = case
+    if kernel == 3 and D == 64:
+        pytest.skip("tiles of 256 rows: heads of 128")
+    S = Sequences(sum(length) + Hq, new, length, H, D, kv).upload()
+    q = queries(S, Hq, act)
+    for blocks in (0, 1, 2):                                                # as it comes, and cut into parts of so many
+        forced(kernel, blocks)
+        out = B.qg_kv_attention(q, S.cache, *S.args, D ** -0.5, max(new), max(length), causal=causal, window=window)
+        check(S, q, out, act, causal, window, D ** -0.5)
+
+
+@pytest.mark.parametrize("kernel", [2, 3])
+@pytest.mark.parametrize("kv", ["i8", "e4m3"])
+def test_tiled_kernel_where_it_can_go_wrong(kernel, kv, forced):
+    """Blocks that are not there, codes past the end that are NaN, a spoilt block, large scores, scales far apart."""
+    from paper_2504_12984_amd import binding as B
+    from oracle import layer_oracle as LO
+    S = Sequences(40, [150, 20], [400, 129], 2, 128, kv, missing=[(0, 1), (0, 4), (1, 0)])
+    for i, e in ((0, -4), (2, -34), (3, 0), (5, -14)):
+        S.scale["v"][S.table[0, i]] = 2.0 ** e
+    if kv == "e4m3":
+        for b in (0, 1):
+            last = S.table[b, (S.length[b] - 1) // 64]
+            for name in "kv":
+                S.codes[name][last][:, LO.order(name, 128)[S.length[b] % 64:].ravel()] = 0x7F
+    S.upload()
+    S.codes = {n: np.where((c & 0x7F) == 0x7F, 0, c) if kv == "e4m3" else c for n, c in S.codes.items()}
+    for std in (1.0, 20.0):
+        q = queries(S, 6, "bf16", std=std)
+        for blocks in (0, 1, 3):
+            forced(kernel, blocks)
+            check(S, q, B.qg_kv_attention(q, S.cache, *S.args, 0.1, 150, 400), "bf16", True, 0, 0.1)
+    S = Sequences(41, [150], [200], 2, 128, kv)
+    for name in "kv":
+        S.scale[name][S.table[0, 2], 1] = np.nan
+        S.upload()
+        q = queries(S, 4, "f16")
+        for blocks in (0, 1):
+            forced(kernel, blocks)
+            bad = torch.isnan(B.qg_kv_attention(q, S.cache, *S.args, 0.1, 150, 200, window=30)).all(-1).cpu().numpy()
+            pos = 50 + np.arange(150)
+            sees = (pos >= 128) & (pos - 30 < 191)
+            assert np.array_equal(bad[:, 2:], np.repeat(sees[:, None], 2, 1)) and not bad[:, :2].any()
+        S.scale[name][S.table[0, 2], 1] = 0.01
+
+
+def test_kernels_agree_and_repeat(forced):
+    from paper_2504_12984_amd import binding as B
+    S = Sequences(42, [300, 5], [900, 700], 2, 128, "i8").upload()
+    q = queries(S, 8, "f16")
+    got = []
+    for kernel in KERNELS:
+        for blocks in (0, 2):
+            forced(kernel, blocks)
+            out = B.qg_kv_attention(q, S.cache, *S.args, 0.09, 300, 900)
+            assert torch.equal(out, B.qg_kv_attention(q, S.cache, *S.args, 0.09, 300, 900))
+            got.append(out)
+    for out in got:
+        assert (out.double() - got[0].double()).abs().max() <= 2.0 ** -9 * got[0].double().abs().max()
+
+
+def test_automatic_choice_of_the_tiled_kernel():
+    """Enough rows that tiles are chosen: of 128 (heads of 64) and of 256 rows."""
+    from paper_2504_12984_amd import binding as B
+    for D, H, Hq, rows in ((64, 8, 8, 2100), (128, 8, 64, 2050)):
+        S = Sequences(43, [rows], [rows + 30], H, D, "i8").upload()
+        q = queries(S, Hq, "bf16")
+        out = B.qg_kv_attention(q, S.cache, *S.args, D ** -0.5, rows, rows + 30)
+        k, there = S.values("k", 0)
+        v, _ = S.values("v", 0)
+        from oracle import layer_oracle as LO
+        for j in (0, 1, 63, 64, 1000, rows - 1):
+            want, weight, reach = LO.attention(f64(q[j:j + 1]), k, v, there, 30 + j, D ** -0.5, True, 0)
+            rel = 2 * reach * (D + 16) * 2.0 ** -24 + 2.0 ** -11 + 2.0 ** -12
+            tol = ROUND["bf16"] * np.abs(want) * (1 + rel) + weight * rel + (rows + 30) * 2.0 ** -25 * np.abs(v).max() + LEAST["bf16"]
+            assert np.all(np.abs(f64(out[j:j + 1]) - want) <= tol)
+
+
+def test_a_forced_kernel_that_does_not_exist(forced):
+    from paper_2504_12984_amd import binding as B
+    S = Sequences(44, [2], [2], 2, 64, "i8").upload()
+    q = torch.zeros(2, 4, 64, dtype=torch.float16).cuda()
+    for kernel in (3, 4, -1):
+        forced(kernel)
+        with pytest.raises(B.QgError):
+            B.qg_kv_attention(q, S.cache, *S.args, 0.1, 2)
+
+
 @pytest.mark.parametrize("rows", [1, 3, 40])
 @pytest.mark.parametrize("kv", ["i8", "e4m3"])
 def test_blocks_that_are_not_there_are_not_seen(rows, kv):
