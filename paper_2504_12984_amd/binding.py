@@ -376,40 +376,44 @@ class BoundQgemmCodebook:
 KV_BLOCK = 64
 
 
-def _rows(t, name, dtype=None):
-    """A CUDA tensor whose rows are contiguous and lie at a stride that only grows: (pointer, row stride)."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda) or t.dtype not in _DT or (dtype is not None and t.dtype != dtype):
-        raise ValueError(f"{name} must be an fp16 or bf16 CUDA tensor of the call's type")
-    if t.stride(-1) != 1 or (t.dim() == 3 and t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+def _rows(t, name, shape, dtype):
+    """A CUDA tensor of this shape and type whose rows (all dimensions but the first) are contiguous: (pointer, row stride)."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.shape == shape):
+        raise ValueError(f"{name} must be a CUDA tensor {list(shape)} of {dtype}")
+    stride = t.stride()
+    width = shape[-1]
+    if (stride[-1] != 1 and width > 1) or (len(shape) == 3 and stride[1] != width and shape[1] > 1):
         raise ValueError(f"{name} must have contiguous rows")
-    width = t.shape[-1] if t.dim() == 2 else t.shape[1] * t.shape[2]
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), width)
+    if shape[0] > 1:
+        return t.data_ptr(), stride[0]
+    return t.data_ptr(), max(stride[0], width if len(shape) == 2 else width * shape[1])
+
+
+def _act(t, name, dims):
+    if not isinstance(t, torch.Tensor) or t.dim() != dims or t.dtype not in _DT:
+        raise ValueError(f"{name} must be an fp16 or bf16 tensor of {dims} dimensions")
+    return t.dtype, t.shape
 
 
 def qg_rmsnorm_a8(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: torch.Tensor | None = None,
                   sum_out: torch.Tensor | None = None):
     """int8 rows of the norm of h = x + residual for qgemm_a8: (A8 int8 [M,N], a_scale fp32 [M], h).  h is x's type, in
     `sum_out` if that is given (`residual` itself is fine); without a residual it is x and nothing is written."""
-    if x.dim() != 2:
-        raise ValueError("x must be [M,N] fp16 or bf16")
-    M, N = x.shape
-    x_ptr, x_stride = _rows(x, "x")
-    if weight.dtype != x.dtype or tuple(weight.shape) != (N,):
+    dtype, shape = _act(x, "x", 2)
+    M, N = shape
+    x_ptr, x_stride = _rows(x, "x", shape, dtype)
+    if weight.dtype is not dtype or weight.shape != (N,):
         raise ValueError("weight must be [N] of x's type")
     r_ptr, r_stride, s_ptr, s_stride = None, 0, None, 0
     if residual is not None:
-        if tuple(residual.shape) != (M, N):
-            raise ValueError("residual must be [M,N] of x's type")
-        r_ptr, r_stride = _rows(residual, "residual", x.dtype)
+        r_ptr, r_stride = _rows(residual, "residual", shape, dtype)
         if sum_out is None:
-            sum_out = torch.empty((M, N), dtype=x.dtype, device=x.device)
+            sum_out = torch.empty_like(x, memory_format=torch.contiguous_format)
     if sum_out is not None:
-        if tuple(sum_out.shape) != (M, N):
-            raise ValueError("sum_out must be [M,N] of x's type")
-        s_ptr, s_stride = _rows(sum_out, "sum_out", x.dtype)
-    A8 = torch.empty((M, N), dtype=torch.int8, device=x.device)
-    a_scale = torch.empty(M, dtype=torch.float32, device=x.device)
-    _check("qg_rmsnorm_a8", _lib.qg_rmsnorm_a8(x_ptr, r_ptr, _ptr(weight, "weight"), eps, _DT[x.dtype], M, N, x_stride, r_stride,
+        s_ptr, s_stride = _rows(sum_out, "sum_out", shape, dtype)
+    A8 = torch.empty_like(x, dtype=torch.int8, memory_format=torch.contiguous_format)
+    a_scale = x.new_empty(M, dtype=torch.float32)
+    _check("qg_rmsnorm_a8", _lib.qg_rmsnorm_a8(x_ptr, r_ptr, _ptr(weight, "weight"), eps, _DT[dtype], M, N, x_stride, r_stride,
                                                A8.data_ptr(), a_scale.data_ptr(), s_ptr, s_stride, _stream()))
     return A8, a_scale, x if sum_out is None else sum_out
 
@@ -417,22 +421,19 @@ def qg_rmsnorm_a8(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: t
 def qg_silu_a8(gate: torch.Tensor, up: torch.Tensor | None = None):
     """int8 rows of silu(gate) * up for qgemm_a8: (A8 int8 [M,N], a_scale fp32 [M]).  With one argument [M, 2N] its first
     half is the gate."""
-    if gate.dim() != 2 or (up is None and gate.shape[1] % 2):
-        raise ValueError("gate must be [M,N], or [M,2N] with the up half behind it")
+    dtype, shape = _act(gate, "gate", 2)
+    M, N = shape
+    g_ptr, g_stride = _rows(gate, "gate", shape, dtype)
     if up is None:
-        N = gate.shape[1] // 2
-        g_ptr, g_stride = _rows(gate, "gate")
+        if N % 2:
+            raise ValueError("gate must be [M,N], or [M,2N] with the up half behind it")
+        N //= 2
         u_ptr, u_stride = g_ptr + 2 * N, g_stride
     else:
-        N = gate.shape[1]
-        if up.shape != gate.shape:
-            raise ValueError("up must be [M,N] of gate's type")
-        g_ptr, g_stride = _rows(gate, "gate")
-        u_ptr, u_stride = _rows(up, "up", gate.dtype)
-    M = gate.shape[0]
-    A8 = torch.empty((M, N), dtype=torch.int8, device=gate.device)
-    a_scale = torch.empty(M, dtype=torch.float32, device=gate.device)
-    _check("qg_silu_a8", _lib.qg_silu_a8(g_ptr, u_ptr, _DT[gate.dtype], M, N, g_stride, u_stride, A8.data_ptr(), a_scale.data_ptr(),
+        u_ptr, u_stride = _rows(up, "up", shape, dtype)
+    A8 = gate.new_empty((M, N), dtype=torch.int8)
+    a_scale = gate.new_empty(M, dtype=torch.float32)
+    _check("qg_silu_a8", _lib.qg_silu_a8(g_ptr, u_ptr, _DT[dtype], M, N, g_stride, u_stride, A8.data_ptr(), a_scale.data_ptr(),
                                          _stream()))
     return A8, a_scale
 
@@ -469,18 +470,12 @@ class KvCache:
 
 def _sequences(row_start, kv_len, block_table):
     """(pointers of the three, table width, batch)"""
-    batch = kv_len.shape[0]
-    if not (row_start.dtype == kv_len.dtype == block_table.dtype == torch.int32):
+    i32, table = torch.int32, block_table.shape
+    if not (row_start.dtype is i32 and kv_len.dtype is i32 and block_table.dtype is i32):
         raise ValueError("row_start, kv_len and block_table must be int32")
-    if row_start.shape != (batch + 1,) or block_table.dim() != 2 or block_table.shape[0] != batch:
+    if len(table) != 2 or kv_len.shape != table[:1] or row_start.shape != (table[0] + 1,):
         raise ValueError("row_start must be [batch + 1], kv_len [batch], block_table [batch, width]")
-    return _ptr(row_start, "row_start"), _ptr(kv_len, "kv_len"), _ptr(block_table, "block_table"), block_table.shape[1], batch
-
-
-def _heads(t, name, rows, heads, dim, dtype):
-    if t.dim() != 3 or tuple(t.shape) != (rows, heads, dim):
-        raise ValueError(f"{name} must be [rows, heads, head_dim] with the cache's head_dim")
-    return _rows(t, name, dtype)
+    return _ptr(row_start, "row_start"), _ptr(kv_len, "kv_len"), _ptr(block_table, "block_table"), table[1], table[0]
 
 
 def qg_kv_append(k: torch.Tensor, v: torch.Tensor, cache: KvCache, row_start: torch.Tensor, kv_len: torch.Tensor,
@@ -490,18 +485,20 @@ def qg_kv_append(k: torch.Tensor, v: torch.Tensor, cache: KvCache, row_start: to
     [positions, rot_dim / 2] if these are given; returns q rotated likewise [rows, q_heads, head_dim], or None without q.
     row_start int32 [batch + 1], kv_len int32 [batch] (new rows included), block_table int32 [batch, width]; max_rows: at
     least the most new rows of one sequence."""
-    rows, D = k.shape[0], cache.head_dim
-    if k.dtype not in _DT:
-        raise ValueError("k must be fp16 or bf16")
-    k_ptr, k_stride = _heads(k, "k", rows, cache.kv_heads, D, k.dtype)
-    v_ptr, v_stride = _heads(v, "v", rows, cache.kv_heads, D, k.dtype)
+    dtype, shape = _act(k, "k", 3)
+    rows, D = shape[0], cache.head_dim
+    if shape[1:] != (cache.kv_heads, D):
+        raise ValueError("k must be [rows, kv_heads, head_dim] with the cache's kv_heads and head_dim")
+    k_ptr, k_stride = _rows(k, "k", shape, dtype)
+    v_ptr, v_stride = _rows(v, "v", shape, dtype)
     q_ptr, q_stride, q_heads = None, 0, 0
     if q is not None:
         q_heads = q.shape[1] if q.dim() == 3 else 0
-        q_ptr, q_stride = _heads(q, "q", rows, q_heads, D, k.dtype)
+        shape = torch.Size((rows, q_heads, D))
+        q_ptr, q_stride = _rows(q, "q", shape, dtype)
         if q_out is None:
-            q_out = torch.empty((rows, q_heads, D), dtype=k.dtype, device=k.device)
-        elif q_out.shape != q.shape or q_out.dtype != q.dtype:
+            q_out = k.new_empty(shape)
+        elif q_out.shape != shape or q_out.dtype is not dtype:
             raise ValueError("q_out must be q's shape and type")
     positions, rot = 0, 0
     if cos is not None or sin is not None:
@@ -510,7 +507,7 @@ def qg_kv_append(k: torch.Tensor, v: torch.Tensor, cache: KvCache, row_start: to
         positions, rot = cos.shape[0], 2 * cos.shape[1]
     s_ptr, l_ptr, t_ptr, width, batch = _sequences(row_start, kv_len, block_table)
     _check("qg_kv_append", _lib.qg_kv_append(
-        q_ptr, k_ptr, v_ptr, _DT[k.dtype], q_stride, k_stride, v_stride, _ptr(cos, "cos"), _ptr(sin, "sin"), positions, rot,
+        q_ptr, k_ptr, v_ptr, _DT[dtype], q_stride, k_stride, v_stride, _ptr(cos, "cos"), _ptr(sin, "sin"), positions, rot,
         int(neighbours), s_ptr, l_ptr, t_ptr, width, batch, rows, max_rows, q_heads, cache.kv_heads, D, cache.type, cache.blocks,
         *cache.ptrs, None if q is None else _ptr(q_out, "q_out"), _stream()))
     return None if q is None else q_out
@@ -521,18 +518,18 @@ def qg_kv_attention(q: torch.Tensor, cache: KvCache, row_start: torch.Tensor, kv
                     out: torch.Tensor | None = None) -> torch.Tensor:
     """Attention of q [rows, q_heads, head_dim] over the cache (arguments as for qg_kv_append; the rows are the last tokens of
     their sequences).  max_kv: at least the longest kv_len (0: as long as the table is wide)."""
-    D = cache.head_dim
-    if q.dim() != 3:
-        raise ValueError("q must be [rows, heads, head_dim]")
-    rows, q_heads = q.shape[:2]
-    q_ptr, q_stride = _heads(q, "q", rows, q_heads, D, None)
+    dtype, shape = _act(q, "q", 3)
+    rows, q_heads, D = shape
+    if D != cache.head_dim:
+        raise ValueError("q must be [rows, heads, head_dim] with the cache's head_dim")
+    q_ptr, q_stride = _rows(q, "q", shape, dtype)
     if out is None:
-        out = torch.empty((rows, q_heads, D), dtype=q.dtype, device=q.device)
-    elif out.shape != q.shape or out.dtype != q.dtype:
+        out = q.new_empty(shape)
+    elif out.shape != shape or out.dtype is not dtype:
         raise ValueError("out must be q's shape and type")
     s_ptr, l_ptr, t_ptr, width, batch = _sequences(row_start, kv_len, block_table)
     _check("qg_kv_attention", _lib.qg_kv_attention(
-        q_ptr, _DT[q.dtype], q_stride, *cache.ptrs, cache.type, cache.blocks, s_ptr, l_ptr, t_ptr, width, batch, rows, max_rows,
+        q_ptr, _DT[dtype], q_stride, *cache.ptrs, cache.type, cache.blocks, s_ptr, l_ptr, t_ptr, width, batch, rows, max_rows,
         max_kv, q_heads, cache.kv_heads, D, scale, int(causal), window, _ptr(out, "out"), _stream()))
     return out
 
