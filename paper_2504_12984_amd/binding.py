@@ -538,11 +538,12 @@ def qg_kv_dequant(cache: KvCache, row_start: torch.Tensor, kv_len: torch.Tensor,
                   dtype: torch.dtype, max_rows: int | None = None):
     """The cache's values of the last row_start[b+1] - row_start[b] tokens of each sequence: k, v [rows, kv_heads, head_dim]."""
     shape = (rows, cache.kv_heads, cache.head_dim)
-    k, v = (torch.empty(shape, dtype=dtype, device=cache.k.device) for _ in range(2))
+    k = cache.k.new_empty(shape, dtype=dtype)
+    v = torch.empty_like(k)
     s_ptr, l_ptr, t_ptr, width, batch = _sequences(row_start, kv_len, block_table)
     _check("qg_kv_dequant", _lib.qg_kv_dequant(
         *cache.ptrs, cache.type, cache.blocks, s_ptr, l_ptr, t_ptr, width, batch, rows, rows if max_rows is None else max_rows,
-        cache.kv_heads, cache.head_dim, _DT[dtype], _ptr(k, "k"), _ptr(v, "v"), _stream()))
+        cache.kv_heads, cache.head_dim, _DT[dtype], k.data_ptr(), v.data_ptr(), _stream()))
     return k, v
 
 

@@ -9,7 +9,12 @@
 
 namespace qg {
 
-constexpr int KV_THREADS = 256;
+// A thread to 16 elements of a block: two would take so many registers that three wavefronts fit a SIMD, not five.
+template <int D>
+constexpr int KV_THREADS = 4 * D;
+// A block's bytes in LDS: 16 more behind each 1024, so that the same byte of neighbouring groups of 16 dimensions, which neighbouring
+// lanes touch, does not lie in one bank (reading a block's values byte by byte: eight lanes to a bank without).
+__host__ __device__ constexpr int in_lds(int byte) { return byte + byte / 1024 * 16; }
 
 // Blocks that `rows` rows at the end of `length` tokens touch (rows before token 0 or past the table are nowhere).
 struct Touched { int first, count, from, upto; };       // blocks first .. first + count - 1, tokens from .. upto - 1
@@ -76,19 +81,34 @@ __device__ __forceinline__ float rotated(const KvParams& p, const uint16_t* head
 }
 
 // Sixteen elements from dimension d0 on (a multiple of 16).  Wide rows: 16-byte loads, and a rotation whose partners of 16
-// neighbouring elements are 16 neighbouring ones too (or the same).
+// neighbouring elements are 16 neighbouring ones too (or the same).  Loads apart from the rest: they need no position.
+struct Raw { uint4 own[2], other[2]; };
+__device__ __forceinline__ Raw load_sixteen(const KvParams& p, const uint16_t* head, int d0, bool rotate) {
+  Raw r = {};
+  if (!p.wide) return r;
+  const uint4* at = reinterpret_cast<const uint4*>(head + d0);
+  r.own[0] = at[0]; r.own[1] = at[1];
+  if (rotate && !p.neighbours && d0 < p.rot) {
+    at = reinterpret_cast<const uint4*>(head + (d0 >= p.rot / 2 ? d0 - p.rot / 2 : d0 + p.rot / 2));
+    r.other[0] = at[0]; r.other[1] = at[1];
+  }
+  return r;
+}
+template <bool BF16>
+__device__ __forceinline__ void unpack16(const uint4 (&u)[2], float (&x)[16]) {
+  float a[8], b[8];
+  unpack8<BF16>(u[0], a); unpack8<BF16>(u[1], b);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) { x[e] = a[e]; x[8 + e] = b[e]; }
+}
 template <bool BF16, bool ROTATE>
-__device__ __forceinline__ void sixteen(const KvParams& p, const uint16_t* head, int d0, int64_t pos, float (&x)[16]) {
+__device__ __forceinline__ void sixteen(const KvParams& p, const Raw& raw, const uint16_t* head, int d0, int64_t pos, float (&x)[16]) {
   if (!p.wide) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = ROTATE ? rotated<BF16>(p, head, d0 + e, pos) : act_to_f32<BF16>(head[d0 + e]);
     return;
   }
-  float a[8], b[8];
-  const uint4* at = reinterpret_cast<const uint4*>(head + d0);
-  unpack8<BF16>(at[0], a); unpack8<BF16>(at[1], b);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) { x[e] = a[e]; x[8 + e] = b[e]; }
+  unpack16<BF16>(raw.own, x);
   if (!ROTATE || d0 >= p.rot) return;
   const int half = p.rot / 2;
   if (p.neighbours) {
@@ -111,10 +131,7 @@ __device__ __forceinline__ void sixteen(const KvParams& p, const uint16_t* head,
     const bool second = d0 >= half;
     const int pair = second ? d0 - half : d0;
     float y[16];
-    at = reinterpret_cast<const uint4*>(head + (second ? d0 - half : d0 + half));
-    unpack8<BF16>(at[0], a); unpack8<BF16>(at[1], b);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) { y[e] = a[e]; y[8 + e] = b[e]; }
+    unpack16<BF16>(raw.other, y);
     const float4* c = reinterpret_cast<const float4*>(p.cos + pos * half + pair);
     const float4* s = reinterpret_cast<const float4*>(p.sin + pos * half + pair);
 #pragma unroll
@@ -146,36 +163,43 @@ __device__ __forceinline__ void four_numbers(uint32_t u, float (&x)[4]) {
   }
 }
 
-// Queries: a workgroup per row.
+// Queries: a workgroup per row.  The first piece is on its way before the row's sequence is known.
 template <int D, bool BF16>
 __device__ __forceinline__ void rotate_queries(const KvParams& p, int row, int l) {
+  const int pieces = p.q_heads * (D / 16);
+  const bool rotate = p.cos != nullptr;
+  const uint16_t* const q = p.q + (int64_t)row * p.q_stride;
+  int i = threadIdx.x;
+  Raw raw = {};
+  if (i < pieces) raw = load_sixteen(p, q + i / (D / 16) * D, i % (D / 16) * 16, rotate);
   const int b = find_sequence(p, row, l);
   if (b < 0) return;
   const Sequence s = sequence(p, b);
   if (row < s.first || row - s.first >= s.rows) return;
   const int64_t pos = min(max((int64_t)s.before + (row - s.first), (int64_t)0), max(p.positions - 1, (int64_t)0));
-  const int pieces = p.q_heads * (D / 16);
-  for (int i = threadIdx.x; i < pieces; i += KV_THREADS) {
-    // partners are read before anything of the head is written: the output may be the input
+  while (i < pieces) {
+    // partners are read before anything of the head is written: the output may be the input, and a head is one wavefront's
     float x[16];
-    const uint16_t* head = p.q + (int64_t)row * p.q_stride + (i / (D / 16)) * D;
-    if (p.cos) sixteen<BF16, true>(p, head, (i % (D / 16)) * 16, pos, x);
-    else       sixteen<BF16, false>(p, head, (i % (D / 16)) * 16, pos, x);
+    const uint16_t* head = q + i / (D / 16) * D;
+    if (rotate) sixteen<BF16, true>(p, raw, head, i % (D / 16) * 16, pos, x);
+    else        sixteen<BF16, false>(p, raw, head, i % (D / 16) * 16, pos, x);
     float a[8], c[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) { a[e] = x[e]; c[e] = x[8 + e]; }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     uint4* out = reinterpret_cast<uint4*>(p.q_out + ((int64_t)row * p.q_heads * D + i * 16));
     out[0] = pack8<BF16>(a); out[1] = pack8<BF16>(c);
+    i += KV_THREADS<D>;
+    if (i < pieces) raw = load_sixteen(p, q + i / (D / 16) * D, i % (D / 16) * 16, rotate);
   }
 }
 
 template <int D, bool BF16, bool E4M3>
-__global__ __launch_bounds__(KV_THREADS) void append_kernel(KvParams p, int kv_units) {
-  constexpr int BYTES = KV_BLOCK * D, PER = BYTES / 16 / KV_THREADS;         // pieces of 16 elements a thread
+__global__ __launch_bounds__(KV_THREADS<D>) void append_kernel(KvParams p, int kv_units) {
+  constexpr int BYTES = KV_BLOCK * D, PER = BYTES / 16 / KV_THREADS<D>;         // pieces of 16 elements a thread
   constexpr float QMAX = E4M3 ? 448.0f : 127.0f;
-  __shared__ __attribute__((aligned(16))) uint8_t image[BYTES];              // the block as it lies in the cache
-  __shared__ uint32_t most[KV_THREADS / 64];
+  __shared__ __attribute__((aligned(16))) uint8_t image[in_lds(BYTES)];              // the block as it lies in the cache
+  __shared__ uint32_t most[KV_THREADS<D> / 64];
   const int tid = threadIdx.x, l = tid & 63;
   int unit = blockIdx.x;
   if (unit >= kv_units) { rotate_queries<D, BF16>(p, unit - kv_units, l); return; }
@@ -200,13 +224,15 @@ __global__ __launch_bounds__(KV_THREADS) void append_kernel(KvParams p, int kv_u
   uint32_t amax = 0u;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int piece = tid + i * KV_THREADS, token = piece / (D / 16), d0 = piece % (D / 16) * 16;
+    const int piece = tid + i * KV_THREADS<D>, token = piece / (D / 16), d0 = piece % (D / 16) * 16;
     if (token < from || token >= upto) continue;
     const int pos = block * KV_BLOCK + token;
     const int64_t row = s.first + (pos - s.before);
-    if (values) sixteen<BF16, false>(p, p.v + row * p.v_stride + head * D, d0, 0, x[i]);
-    else if (p.cos) sixteen<BF16, true>(p, p.k + row * p.k_stride + head * D, d0, min((int64_t)pos, p.positions - 1), x[i]);
-    else sixteen<BF16, false>(p, p.k + row * p.k_stride + head * D, d0, 0, x[i]);
+    const uint16_t* from_head = (values ? p.v + row * p.v_stride : p.k + row * p.k_stride) + head * D;
+    const bool rotate = !values && p.cos;
+    const Raw raw = load_sixteen(p, from_head, d0, rotate);
+    if (rotate) sixteen<BF16, true>(p, raw, from_head, d0, min((int64_t)pos, p.positions - 1), x[i]);
+    else        sixteen<BF16, false>(p, raw, from_head, d0, 0, x[i]);
 #pragma unroll
     for (int e = 0; e < 16; ++e) amax = max(amax, magnitude(x[i][e]));
   }
@@ -215,7 +241,7 @@ __global__ __launch_bounds__(KV_THREADS) void append_kernel(KvParams p, int kv_u
   if (l == 0) most[tid >> 6] = amax;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < KV_THREADS / 64; ++i) amax = max(amax, most[i]);
+  for (int i = 0; i < KV_THREADS<D> / 64; ++i) amax = max(amax, most[i]);
   float scale = scale_of(amax, QMAX);
   if (from > 0 && !(scale > was) && scale == scale) scale = was;             // also where what was there is NaN
   if (from > 0 && was != was) scale = was;
@@ -226,8 +252,10 @@ __global__ __launch_bounds__(KV_THREADS) void append_kernel(KvParams p, int kv_u
   const bool whole = from == 0 || scale != was;
   if (whole && from > 0) {
     const float move = was * inv;
-    for (int i = tid; i < BYTES / 16; i += KV_THREADS) {
-      uint4 c = reinterpret_cast<const uint4*>(cache)[i];
+#pragma unroll
+    for (int n = 0; n < PER; ++n) {
+      const int i = tid + n * KV_THREADS<D>;
+      const uint4 c = reinterpret_cast<const uint4*>(cache)[i];
       uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -235,33 +263,39 @@ __global__ __launch_bounds__(KV_THREADS) void append_kernel(KvParams p, int kv_u
         four_numbers<E4M3>(w[e], y);
         w[e] = four_codes<E4M3>(y[0] * move, y[1] * move, y[2] * move, y[3] * move);
       }
-      reinterpret_cast<uint4*>(image)[i] = make_uint4(w[0], w[1], w[2], w[3]);
+      *reinterpret_cast<uint4*>(image + in_lds(16 * i)) = make_uint4(w[0], w[1], w[2], w[3]);
     }
     __syncthreads();
   } else if (whole) {
     const uint32_t none = E4M3 ? 0u : 0x80808080u;
-    for (int i = tid; i < BYTES / 16; i += KV_THREADS) reinterpret_cast<uint4*>(image)[i] = make_uint4(none, none, none, none);
+#pragma unroll
+    for (int n = 0; n < PER; ++n) *reinterpret_cast<uint4*>(image + in_lds((tid + n * KV_THREADS<D>) * 16)) = make_uint4(none, none, none, none);
     __syncthreads();
   }
   uint8_t* to = whole ? image : cache;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int piece = tid + i * KV_THREADS, token = piece / (D / 16), d0 = piece % (D / 16) * 16;
+    const int piece = tid + i * KV_THREADS<D>, token = piece / (D / 16), d0 = piece % (D / 16) * 16;
     if (token < from || token >= upto) continue;
     uint32_t w[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       w[e] = four_codes<E4M3>(x[i][4 * e] * inv, x[i][4 * e + 1] * inv, x[i][4 * e + 2] * inv, x[i][4 * e + 3] * inv);
     if (!values) {
-      *reinterpret_cast<uint4*>(to + key_byte<D>(token, d0)) = make_uint4(w[0], w[1], w[2], w[3]);
+      const int byte = key_byte<D>(token, d0);
+      *reinterpret_cast<uint4*>(to + (whole ? in_lds(byte) : byte)) = make_uint4(w[0], w[1], w[2], w[3]);
     } else {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) to[value_byte(token, d0 + e)] = (uint8_t)(w[e / 4] >> (8 * (e % 4)));
+      for (int e = 0; e < 16; ++e) {
+        const int byte = value_byte(token, d0 + e);
+        to[whole ? in_lds(byte) : byte] = (uint8_t)(w[e / 4] >> (8 * (e % 4)));
+      }
     }
   }
   if (whole) {
     __syncthreads();
-    for (int i = tid; i < BYTES / 16; i += KV_THREADS) reinterpret_cast<uint4*>(cache)[i] = reinterpret_cast<const uint4*>(image)[i];
+#pragma unroll
+    for (int n = 0; n < PER; ++n) reinterpret_cast<uint4*>(cache)[tid + n * KV_THREADS<D>] = *reinterpret_cast<const uint4*>(image + in_lds((tid + n * KV_THREADS<D>) * 16));
     if (tid == 0) *scale_at = scale;
   }
 }
@@ -269,9 +303,9 @@ __global__ __launch_bounds__(KV_THREADS) void append_kernel(KvParams p, int kv_u
 // The values of the last rows of each sequence.  A block's bytes go through LDS: they are read in their order and
 // written in the rows'.
 template <int D, bool BF16, bool E4M3>
-__global__ __launch_bounds__(KV_THREADS) void dequant_kernel_kv(KvParams p) {
-  constexpr int BYTES = KV_BLOCK * D;
-  __shared__ __attribute__((aligned(16))) uint8_t image[BYTES];
+__global__ __launch_bounds__(KV_THREADS<D>) void dequant_kernel_kv(KvParams p) {
+  constexpr int BYTES = KV_BLOCK * D, PER = BYTES / 16 / KV_THREADS<D>;
+  __shared__ __attribute__((aligned(16))) uint8_t image[in_lds(BYTES)];
   const int tid = threadIdx.x, l = tid & 63, unit = blockIdx.x;
   const bool values = unit & 1;
   const int head = (unit >> 1) % p.kv_heads;
@@ -288,24 +322,28 @@ __global__ __launch_bounds__(KV_THREADS) void dequant_kernel_kv(KvParams p) {
   if (there) {
     scale = (values ? p.v_scale : p.k_scale)[(int64_t)id * p.kv_heads + head];
     const uint8_t* cache = (values ? p.v_cache : p.k_cache) + ((int64_t)id * p.kv_heads + head) * BYTES;
-    for (int i = tid; i < BYTES / 16; i += KV_THREADS) reinterpret_cast<uint4*>(image)[i] = reinterpret_cast<const uint4*>(cache)[i];
+    uint4 c[PER];
+#pragma unroll
+    for (int n = 0; n < PER; ++n) c[n] = reinterpret_cast<const uint4*>(cache)[tid + n * KV_THREADS<D>];
+#pragma unroll
+    for (int n = 0; n < PER; ++n) *reinterpret_cast<uint4*>(image + in_lds((tid + n * KV_THREADS<D>) * 16)) = c[n];
   }
   __syncthreads();
   const int from = max(t.from - block * KV_BLOCK, 0), upto = min(t.upto - block * KV_BLOCK, KV_BLOCK);
   uint16_t* out = values ? p.v_out : p.k_out;
-  for (int i = tid; i < BYTES / 8; i += KV_THREADS) {
-    const int token = i / (D / 8), d0 = i % (D / 8) * 8;
-    if (token < from || token >= upto) continue;
+#pragma unroll
+  for (int n = 0; n < 2 * PER; ++n) {
+    const int i = tid + n * KV_THREADS<D>, token = i / (D / 8), d0 = i % (D / 8) * 8;
     float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (there) {
       uint32_t w[2];
       if (values) {
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-          w[e] = image[value_byte(token, d0 + 4 * e)] | image[value_byte(token, d0 + 4 * e + 1)] << 8 |
-                 image[value_byte(token, d0 + 4 * e + 2)] << 16 | (uint32_t)image[value_byte(token, d0 + 4 * e + 3)] << 24;
+          w[e] = image[in_lds(value_byte(token, d0 + 4 * e))] | image[in_lds(value_byte(token, d0 + 4 * e + 1))] << 8 |
+                 image[in_lds(value_byte(token, d0 + 4 * e + 2))] << 16 | (uint32_t)image[in_lds(value_byte(token, d0 + 4 * e + 3))] << 24;
       } else {
-        const uint2 u = *reinterpret_cast<const uint2*>(image + key_byte<D>(token, d0));
+        const uint2 u = *reinterpret_cast<const uint2*>(image + in_lds(key_byte<D>(token, d0)));
         w[0] = u.x; w[1] = u.y;
       }
       float y[4];
@@ -317,7 +355,7 @@ __global__ __launch_bounds__(KV_THREADS) void dequant_kernel_kv(KvParams p) {
       for (int e = 0; e < 4; ++e) x[4 + e] = y[e] * scale;
     }
     const int64_t row = s.first + (block * KV_BLOCK + token - s.before);
-    *reinterpret_cast<uint4*>(out + (row * p.kv_heads + head) * D + d0) = pack8<BF16>(x);
+    if (token >= from && token < upto) *reinterpret_cast<uint4*>(out + (row * p.kv_heads + head) * D + d0) = pack8<BF16>(x);
   }
 }
 
@@ -326,7 +364,7 @@ static int launch_append(const KvParams& p, hipStream_t st) {
   const int64_t units = most_units(p) * p.kv_heads * 2, grid = units + (p.q ? p.rows : 0);
   if (grid == 0) return QG_OK;
   if (grid > MOST_GROUPS) return QG_EUNSUPPORTED;
-  hipLaunchKernelGGL((append_kernel<D, BF16, E4M3>), dim3((unsigned)grid), dim3(KV_THREADS), 0, st, p, (int)units);
+  hipLaunchKernelGGL((append_kernel<D, BF16, E4M3>), dim3((unsigned)grid), dim3(KV_THREADS<D>), 0, st, p, (int)units);
   return hipGetLastError() == hipSuccess ? QG_OK : QG_EHIP;
 }
 template <int D, bool BF16, bool E4M3>
@@ -334,7 +372,7 @@ static int launch_dequant(const KvParams& p, hipStream_t st) {
   const int64_t units = most_units(p) * p.kv_heads * 2;
   if (units == 0) return QG_OK;
   if (units > MOST_GROUPS) return QG_EUNSUPPORTED;
-  hipLaunchKernelGGL((dequant_kernel_kv<D, BF16, E4M3>), dim3((unsigned)units), dim3(KV_THREADS), 0, st, p);
+  hipLaunchKernelGGL((dequant_kernel_kv<D, BF16, E4M3>), dim3((unsigned)units), dim3(KV_THREADS<D>), 0, st, p);
   return hipGetLastError() == hipSuccess ? QG_OK : QG_EHIP;
 }
 
