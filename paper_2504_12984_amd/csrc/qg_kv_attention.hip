@@ -525,8 +525,11 @@ __global__ __launch_bounds__(64 * W, 2) void tile_kernel(KvParams p) {
   const int tid = threadIdx.x, l = tid & 63, i = l & 31, half = l >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int H = p.kv_heads, G = p.q_heads / H;
-  const int h = blockIdx.x % H, b = blockIdx.x / H % p.batch;
-  const int tile = (int)(gridDim.x / H / p.batch) - 1 - (int)(blockIdx.x / H / p.batch);      // rows that see most start first
+  // Heads go round the XCDs, whose caches hold a head's blocks for all its tiles; then the sequences, tiles that see most first.  The
+  // workgroups of a CU come 32 apart: sequences start at another place for every tile (by the golden section), so that a CU does
+  // not get the same one, which may be the longest, again and again.
+  const int B = p.batch, at = blockIdx.x / H, nth = at / B;
+  const int h = blockIdx.x % H, tile = (int)(gridDim.x / H / B) - 1 - nth, b = (int)((at % B + (int64_t)nth * 79 * B / 128) % B);
   const Sequence s = sequence(p, b);
   const int rows = s.rows * G, r0 = tile * TILE_ROWS;
   if (r0 >= rows) return;
