@@ -37,7 +37,8 @@ extern "C" {
  *   sum_out      [M, N] of `act`, row stride sum_stride: h rounded to nearest even.  May be NULL, may be `residual` or
  *                `x` itself (with its stride); otherwise outputs must not overlap inputs
  *   A8           [M, N] int8, contiguous, 8-byte aligned where N is a multiple of 8;   a_scale  [M] fp32
- * h, the sum and the norm are fp32 (h is not rounded before the norm).  M >= 0, 1 <= N <= 2^24, eps >= 0.
+ * h, the sum and the norm are fp32 (h is not rounded before the norm).  M >= 0 (2^22 rows and more: QG_EUNSUPPORTED),
+ * 1 <= N <= 2^24, eps >= 0.
  * QG_EINVAL on null or misaligned pointers, strides below N, a negative or NaN eps. */
 QG_API int qg_rmsnorm_a8(const void* x, const void* residual, const void* weight, float eps, int act, int64_t M, int64_t N,
                   int64_t x_stride, int64_t residual_stride, int8_t* A8, float* a_scale, void* sum_out, int64_t sum_stride,
@@ -53,7 +54,7 @@ QG_API int qg_silu_a8(const void* gate, const void* up, int act, int64_t M, int6
 /* The paged cache.  A block holds QG_KV_BLOCK tokens of every key/value head; per block and head there are one scale for
  * the keys and one for the values.
  *   k_cache, v_cache   [num_blocks, kv_heads, 64 * head_dim] bytes, 16-byte aligned
- *   k_scale, v_scale   [num_blocks, kv_heads] fp32
+ *   k_scale, v_scale   [num_blocks, kv_heads] fp32, positive (attention reads value scales below the floor as the floor)
  *   type               {QG_INT, 8, 0, 0} (stored offset-binary, as integer weights are) or {QG_FLOAT, 8, 4, 3}
  * Inside a (block, head) bytes lie in the order in which the lanes of a wavefront load them as operands of the 16x16x32
  * matrix instruction, so that neither kernel moves them between lanes:
@@ -99,9 +100,10 @@ QG_API int qg_kv_append(const void* q, const void* k, const void* v, int act, in
  * Scores, softmax statistics and sums are fp32; products run on the fp16 matrix instruction for either `act`: 8-bit codes
  * are exact in it, bf16 queries are brought into its range by a power of two per row, probabilities (times the block's value
  * scale, over the row's largest such) are rounded to it.
- * Few rows per sequence (up to 64 with their heads) stream the cache once, cut along the tokens where sequences and heads alone would not fill
- * the GPU; the parts meet in the workspace that qgemm uses, in a fixed order.  Where no workspace is to be had (see qgemm.h)
- * the call runs uncut. */
+ * Few rows (up to 192 of a sequence and key/value head, counting the query heads that share it, and more in small calls) stream
+ * the cache; more rows share converted blocks in tiles of 128 or 256.  Either is cut along the tokens where sequences, heads and
+ * rows alone would not fill the GPU; the parts meet in the workspace that qgemm uses, in a fixed order.  Where no workspace is
+ * to be had (see qgemm.h) the call runs uncut. */
 QG_API int qg_kv_attention(const void* q, int act, int64_t q_stride, const void* k_cache, const void* v_cache, const float* k_scale,
                     const float* v_scale, qg_wtype type, int64_t num_blocks, const int32_t* row_start, const int32_t* kv_len,
                     const int32_t* block_table, int64_t table_width, int64_t batch, int64_t rows, int64_t max_rows, int64_t max_kv,

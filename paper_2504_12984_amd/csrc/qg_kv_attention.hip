@@ -2,10 +2,10 @@
 //
 //   s_t = scale q . k_t,   out = sum_t exp(s_t) v_t / sum_t exp(s_t)      over the tokens t that a row sees
 //
-// Both kernels compute transposed: scores^T = K Q^T and out^T = V^T P^T with the 16x16x32 matrix instruction, so that a
-// lane holds scores of ONE row of q (column i = lane % 16) and the softmax needs no lane but the three others of that
-// column.  The four scores that lane 16 b + i gets of a 16-token tile are tokens 4 b .. 4 b + 3; a cache block stores its
-// values' tokens in the order that makes these registers the operand of the second product as they are.
+// Both kernels compute transposed: scores^T = K Q^T and out^T = V^T P^T, so that a lane holds scores of ONE row of q and the
+// softmax needs no lane but the few others of that column.  With the 16x16x32 matrix instruction (few rows) the four scores
+// that lane 16 b + i gets of a 16-token tile are tokens 4 b .. 4 b + 3 of row i; a cache block stores its values' tokens in the
+// order that makes these registers the operand of the second product as they are.
 //
 // Codes become fp16 exactly (int8 through 1024 + u, e4m3 by the hardware's convert).  The scales are applied where they
 // cost nothing: the keys' with the softmax's factor, and the values' in the exponent,
@@ -269,8 +269,9 @@ template <int D, int T>
 constexpr int PART = 16 * T * (D + 2);
 
 // Few rows per sequence: the cache is streamed once.  A workgroup takes 16 T rows (query heads of one key/value head,
-// consecutive tokens) and a part of the blocks they see; its wavefronts take every fourth block each, all by themselves,
-// and meet at the end.  Bound: HBM, 2 D bytes a token and head.
+// consecutive tokens) and a part of the blocks they see; its wavefronts take every eighth block each, all by themselves,
+// and meet at the end.  Bound: HBM, 2 D bytes a token and head.  Measured, 128 wide, 64 heads over 8: one row of 64 sequences of
+// 1000 to 8000 tokens 107 us, one row on 131071 tokens 49 us (5.8 and 5.5 TB/s; a kernel that only reads reaches 5.8).
 template <int D, bool BF16, bool E4M3, int T, bool SHARED>
 __global__ __launch_bounds__(64 * STREAM_WAVES, 2) void stream_kernel(KvParams p) {
   constexpr int BYTES = KV_BLOCK * D, LOADS = BYTES / 1024, STREAM_ROWS = 16 * T;
@@ -506,11 +507,12 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, 2) void stream_kernel(KvParams p
   else                         *reinterpret_cast<uint32_t*>(out) = w[0];
 }
 
-// Many rows per sequence: bound by the vector work of the softmax and the matrix instruction, which takes 16 of 32 rows' cycles
-// from it.  A workgroup takes 256 rows (the query heads of one key/value head for consecutive tokens), 32 to a wavefront; a
-// block's codes are converted once for all of them, into LDS in the order in which lanes read operands.  Here the
-// matrix instruction is the 32x32x16 one: half as many of them issue, and a lane holds 32 scores of one row, so that there
-// is one reference and one sum to a lane.  Lane 32 h + i gets the scores of row i and tokens 32 k + 8 g + 4 h + r; as before
+// Many rows per sequence: bound by the issue of the matrix instructions and of the softmax's vector work, which share the SIMD:
+// for 8192 tokens, 64 heads of 128 over 8, the matrix units are busy 0.44 of the time and the vector unit 0.49, 1010 TFLOP/s
+// (a large library product: 1160 to 1220).  A workgroup takes 32 W rows (the query heads of one key/value head for consecutive
+// tokens), 32 to a wavefront; a block's codes are converted once for all of them, into LDS in the order in which lanes read
+// operands.  Here the matrix instruction is the 32x32x16 one: half as many of them issue, and a lane holds 32 scores of one row,
+// so that there is one reference and one sum to a lane.  Lane 32 h + i gets the scores of row i and tokens 32 k + 8 g + 4 h + r; as before
 // they are the second product's operand as they are.
 // Partial results of one wavefront and part: accumulators, reference and sum of every lane.
 template <int D>

@@ -136,7 +136,7 @@ __device__ __forceinline__ Sequence sequence(const KvParams& p, int b) {
 }
 
 // Threads of one grid dimension stay below 2^32.
-constexpr int64_t MOST_GROUPS = 1 << 22;
+constexpr int64_t MOST_GROUPS = (1 << 22) - 1;          // of at most 1024
 
 int layer_norm_launch(const RowsParams&, hipStream_t);
 int layer_gate_launch(const RowsParams&, hipStream_t);

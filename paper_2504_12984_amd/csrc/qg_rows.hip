@@ -169,6 +169,7 @@ __global__ __launch_bounds__(1024) void rows_any_kernel(RowsParams p) {
 // Gate: 1000 x 14336  8x4 14.5, 16x2 14.8;  1000 x 28672  16x4 27.6 (5.2 TB/s).
 template <int OP, bool BF16>
 static int launch_rows(const RowsParams& p, hipStream_t st) {
+  if (p.M > MOST_GROUPS) return QG_EUNSUPPORTED;
   const int vecs = p.N / 8;
 #define QG_ROWS(W, V)                                                                                                    \
   if (p.wide && vecs <= 64 * (W) * (V)) {                                                                                \
