@@ -45,7 +45,8 @@ extern "C" {
  * Knobs 0, 1 and 3 apply to QG_LAYOUT_TILE128x64 only.
  *   knob 4: forced kernel of qg_kv_attention (1 = streaming kernel, 2 / 3 = tiled kernel with 128 / 256 rows; 3 has heads of 128
  *           only, else QG_EINVAL)
- *   knob 5: blocks of the cache to a part of qg_kv_attention, where there is a workspace for the parts */
+ *   knob 5: blocks of the cache to a part of qg_kv_attention, where there is a workspace for the parts; -n = the tiled kernel in
+ *           equal shares of at least n blocks (with knob 4 at 2 for heads of 64, at 3 for heads of 128, else QG_EINVAL) */
 QG_API int qg_set_knob(int knob, int value);
 
 #ifdef __cplusplus

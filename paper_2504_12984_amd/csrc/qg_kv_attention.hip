@@ -14,7 +14,10 @@
 // is near 1, is what the fp16 operand can hold best.
 // The reference m is not the running maximum itself but is only moved when that exceeds it by 8 (P' up to 256): rescaling
 // the accumulators becomes rare.
+#include <cmath>
+
 #include "qg_layer.h"
+#include "qg_wait.h"
 
 namespace qg {
 
@@ -514,11 +517,29 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, 2) void stream_kernel(KvParams p
 // operands.  Here the matrix instruction is the 32x32x16 one: half as many of them issue, and a lane holds 32 scores of one row,
 // so that there is one reference and one sum to a lane.  Lane 32 h + i gets the scores of row i and tokens 32 k + 8 g + 4 h + r; as before
 // they are the second product's operand as they are.
-// Partial results of one wavefront and part: accumulators, reference and sum of every lane.
+//
+// A tile's blocks may be cut into pieces, in one of two ways.  Either the grid has a second dimension of parts, each of the same
+// number of blocks, for calls with too few tiles to fill the GPU.  Or (SHARES) all tiles of a head, one after the other, are cut
+// into equal shares, one to each workgroup that the GPU holds at once, for tiles that would fill it once and a bit.  Pieces are
+// put together by the wavefront that comes last to its 32 rows; the others leave their results in the workspace.
+// Partial results of one wavefront: accumulators, reference and sum of every lane.
 template <int D>
 constexpr int TILE_PART = 64 * (D / 2 + 2);
-template <int D, bool BF16, bool E4M3, int W>
-__global__ __launch_bounds__(64 * W, 2) void tile_kernel(KvParams p) {
+
+// What a tile costs: its blocks and one more (0: there is no such tile).  c counts a head's tiles, `tiles` to a sequence.
+template <int TILE_ROWS>
+__device__ __forceinline__ int tile_cost(const KvParams& p, int G, int c, int tiles) {
+  if (c >= tiles * p.batch) return 0;
+  const Sequence s = sequence(p, c / tiles);
+  const int rows = s.rows * G, r0 = c % tiles * TILE_ROWS;
+  if (r0 >= rows) return 0;
+  const int length = (int)min((int64_t)max(s.length, 0), p.width * KV_BLOCK);
+  const int from = seen(p, s.before + r0 / G, length).lo, upto = seen(p, s.before + min(r0 + TILE_ROWS - 1, rows - 1) / G, length).hi;
+  return (upto > from ? (upto - 1) / KV_BLOCK + 1 - from / KV_BLOCK : 0) + 1;
+}
+
+template <int D, bool BF16, bool E4M3, int W, bool SHARES>
+__global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void tile_kernel(KvParams p) {
   constexpr int TILE_ROWS = 32 * W;
   constexpr int BYTES = KV_BLOCK * D, PIECES = BYTES / 16, FRAGS = BYTES * 2 / 1024;
   constexpr int EACH = PIECES / (64 * W);                    // pieces of keys, and of values, that a thread converts ...
@@ -527,23 +548,75 @@ __global__ __launch_bounds__(64 * W, 2) void tile_kernel(KvParams p) {
   const int tid = threadIdx.x, l = tid & 63, i = l & 31, half = l >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int H = p.kv_heads, G = p.q_heads / H;
-  // Heads go round the XCDs, whose caches hold a head's blocks for all its tiles; then the sequences, tiles that see most first.  The
-  // workgroups of a CU come 32 apart: sequences start at another place for every tile (by the golden section), so that a CU does
-  // not get the same one, which may be the longest, again and again.
-  const int B = p.batch, at = blockIdx.x / H, nth = at / B;
-  const int h = blockIdx.x % H, tile = (int)(gridDim.x / H / B) - 1 - nth, b = (int)((at % B + (int64_t)nth * 79 * B / 128) % B);
+  // Heads go round the XCDs, whose caches hold a head's blocks for all its tiles.
+  const int B = p.batch, h = blockIdx.x % H, group = blockIdx.x / H;
+  const int tiles = (int)(((int64_t)p.max_rows * G + TILE_ROWS - 1) / TILE_ROWS);
+  // a share: from `at` to `at_end` of all tiles' costs; tiles before the one looked for: c0, of cost `before` together
+  int each = 0, at = 0, at_end = 1, c0 = 0, before = 0;
+  if constexpr (SHARES) {
+    int total = 0;
+    for (int c = 0; c < tiles * B; c += 64) total += tile_cost<TILE_ROWS>(p, G, c + l, tiles);
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) total += __shfl_xor(total, m);
+    total = __builtin_amdgcn_readfirstlane(total);
+    each = max((total + p.splits - 1) / p.splits, p.least);
+    at = group * each;
+    at_end = min(at + each, total);
+  }
+  while (at < at_end) {
+  int b, tile, skipped = 0, cost = 0;
+  if constexpr (SHARES) {
+    for (;;) {
+      if (c0 >= tiles * B) return;                              // (no: there is a tile at each cost below the total)
+      const int mine = tile_cost<TILE_ROWS>(p, G, c0 + l, tiles);
+      int sum = mine;                                           // of the lanes up to this one
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const int x = __shfl_up(sum, d);
+        if (l >= d) sum += x;
+      }
+      const uint64_t over = __ballot(before + sum > at);
+      if (over) {
+        const int lane = __builtin_ctzll(over);
+        b = (c0 + lane) / tiles; tile = (c0 + lane) % tiles;
+        cost = __builtin_amdgcn_readlane(mine, lane);
+        skipped = at - (before + __builtin_amdgcn_readlane(sum, lane) - cost);
+        break;
+      }
+      before += __builtin_amdgcn_readlane(sum, 63);
+      c0 += 64;
+    }
+  } else {
+    // A workgroup to a tile: tiles that see most first.  The workgroups of a CU come 32 apart: sequences start at another place for
+    // every tile (by the golden section), so that a CU does not get the same one, which may be the longest, again and again.
+    const int nth = group / B;
+    tile = tiles - 1 - nth; b = (int)((group % B + (int64_t)nth * 79 * B / 128) % B);
+  }
   const Sequence s = sequence(p, b);
   const int rows = s.rows * G, r0 = tile * TILE_ROWS;
-  if (r0 >= rows) return;
+  if (!SHARES && r0 >= rows) return;
   const int length = (int)min((int64_t)max(s.length, 0), p.width * KV_BLOCK);
   const auto place = [&](int row) { return s.before + min(row, rows - 1) / G; };
   const int from = seen(p, place(r0), length).lo, upto = seen(p, place(r0 + TILE_ROWS - 1), length).hi;
   const int all = upto > from ? (upto - 1) / KV_BLOCK + 1 - from / KV_BLOCK : 0;
-  // p.splits: blocks to a part, as in the streaming kernel
-  const int each = max(p.splits, (int)((all + gridDim.y - 1) / gridDim.y));
-  const int parts = max((all + each - 1) / each, 1), part = blockIdx.y;
-  if (part >= parts) return;
-  const int first = from / KV_BLOCK + part * each, end = min(first + each, from / KV_BLOCK + all);
+  // this piece of the tile, the piece'th of `pieces`, and the tile's places in the workspace: place0, place0 + step, ...
+  int first = from / KV_BLOCK, end = first + all, pieces, piece, place0, step;
+  if constexpr (SHARES) {
+    const int start = at - skipped, stop = start + cost, group0 = start / each;
+    pieces = (stop - 1) / each + 1 - group0; piece = group - group0;
+    place0 = group0 * H + h; step = H;
+    end = first + min(min(stop, at_end) - start, all);
+    first += min(skipped, all);
+    at = min(stop, at_end);
+  } else {
+    const int part = max(p.splits, (int)((all + gridDim.y - 1) / gridDim.y));
+    pieces = max((all + part - 1) / part, 1); piece = blockIdx.y;
+    if (piece >= pieces) return;
+    place0 = blockIdx.x * gridDim.y; step = 1;
+    first += piece * part;
+    end = min(first + part, end);
+    at = at_end;
+  }
   // the wavefront's own rows: seen by some of them, by all of them
   const int w0 = r0 + wave * 32, row = w0 + i;
   const Seen seeA = seen(p, place(w0), length), seeZ = seen(p, place(w0 + 31), length);
@@ -673,48 +746,72 @@ __global__ __launch_bounds__(64 * W, 2) void tile_kernel(KvParams p) {
     }
   }
   float L = half_sum(st.l);
-  if (parts > 1) {
-    // A wavefront's parts meet by themselves, in the order of the tokens: accumulators lie in the workspace as in the lanes.
-    if (w0 >= rows) return;
+  if (w0 >= rows) continue;
+  if (pieces > 1) {
+    // A wavefront's pieces meet by themselves.  Who is not the last to come leaves its results, as they lie in the lanes; the last
+    // one, which at most waits for others' stores, adds all up in the order of the tokens.
     constexpr int SIZE = TILE_PART<D>, PAIRS = D / 4;
-    float* const mine = p.partial + (((int64_t)blockIdx.x * gridDim.y) * W + wave) * SIZE;
-    const auto slot = [&](int k, int pair) { return reinterpret_cast<unsigned long long*>(mine + (int64_t)k * W * SIZE) + pair * 64 + l; };
     const auto two = [](float x, float y) { return __builtin_bit_cast(uint32_t, x) | (unsigned long long)__builtin_bit_cast(uint32_t, y) << 32; };
     const auto lower = [](unsigned long long u) { return __builtin_bit_cast(float, (uint32_t)u); };
     const auto upper = [](unsigned long long u) { return __builtin_bit_cast(float, (uint32_t)(u >> 32)); };
-#pragma unroll
-    for (int n = 0; n < PAIRS; ++n)
-      __hip_atomic_store(slot(part, n), two(o[n / 8][n % 8 * 2], o[n / 8][n % 8 * 2 + 1]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __hip_atomic_store(slot(part, PAIRS), two(st.m, L), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    unsigned* ticket = p.tickets + ((int64_t)blockIdx.x * W + wave) * p.stride;
+    const auto at_place = [&](int n) { return (place0 + (int64_t)n * step) * W + wave; };
+    const auto pair_of = [&](int place, int n) { return reinterpret_cast<unsigned long long*>(p.partial + at_place(place) * SIZE) + n * 64 + l; };
+    // which place a piece took: a share ends with one that is a first piece, and begins with one that is not
+    unsigned* const taken = reinterpret_cast<unsigned*>(p.partial + (int64_t)gridDim.x * gridDim.y * W * SIZE);
+    const auto taken_by = [&](int k) { return taken + 2 * at_place(k) + (k == 0); };
+    unsigned* const ticket = p.tickets + ((int64_t)(SHARES ? place0 : (int)blockIdx.x) * W + wave) * p.stride;
     unsigned came = 0;
     if (l == 0) came = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (__builtin_amdgcn_readfirstlane(came) != (unsigned)(parts - 1)) return;
+    came = __builtin_amdgcn_readfirstlane(came) & 0xffffu;
+    if (came != (unsigned)(pieces - 1)) {
+#pragma unroll
+      for (int n = 0; n < PAIRS; ++n)
+        __hip_atomic_store(pair_of(came, n), two(o[n / 8][n % 8 * 2], o[n / 8][n % 8 * 2 + 1]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(pair_of(came, PAIRS), two(st.m, L), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (l == 0) __hip_atomic_store(taken_by(piece), came, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // they are out before they count
+      if (l == 0) __hip_atomic_fetch_add(ticket, 0x10000u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      continue;
+    }
+    (void)wait_for([&] { return __builtin_amdgcn_readfirstlane(__hip_atomic_load(ticket, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) >> 16; },
+                   (unsigned)(pieces - 1), [] { __builtin_amdgcn_s_sleep(1); });
+    asm volatile("" ::: "memory");                              // nothing is read ahead of the count
     if (l == 0) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    float M = NONE;
-    for (int k = 0; k < parts; ++k) M = fmaxf(M, lower(__hip_atomic_load(slot(k, PAIRS), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)));
-    L = 0.0f;
+    float16v x[D / 32];
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
-    for (int k = 0; k < parts; ++k) {
-      unsigned long long u[PAIRS];
-      const unsigned long long ml = __hip_atomic_load(slot(k, PAIRS), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      for (int r = 0; r < 16; ++r) x[d][r] = 0.0f;
+    float M = NONE, sum = 0.0f;
+    unsigned took = 0;
+    for (int k = 0; k < pieces; ++k) {
+      if (k % 64 == 0 && k + l < pieces && k + l != piece) took = __hip_atomic_load(taken_by(k + l), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      unsigned long long ml = two(st.m, L), u[PAIRS];
+      if (k == piece) {
 #pragma unroll
-      for (int n = 0; n < PAIRS; ++n) u[n] = __hip_atomic_load(slot(k, n), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      const float f = M == NONE ? 1.0f : __builtin_amdgcn_exp2f(lower(ml) - M);
-      L = fmaf(f, upper(ml), L);
+        for (int n = 0; n < PAIRS; ++n) u[n] = two(o[n / 8][n % 8 * 2], o[n / 8][n % 8 * 2 + 1]);
+      } else {
+        const int place = min(__builtin_amdgcn_readlane(took, k % 64), (unsigned)(pieces - 2));
+        ml = __hip_atomic_load(pair_of(place, PAIRS), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+        for (int n = 0; n < PAIRS; ++n) u[n] = __hip_atomic_load(pair_of(place, n), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+      const float top = fmaxf(M, lower(ml));
+      const float back = top == NONE ? 1.0f : __builtin_amdgcn_exp2f(M - top), f = top == NONE ? 1.0f : __builtin_amdgcn_exp2f(lower(ml) - top);
+      M = top;
+      sum = fmaf(f, upper(ml), sum * back);
 #pragma unroll
       for (int n = 0; n < PAIRS; ++n) {
-        o[n / 8][n % 8 * 2] = fmaf(f, lower(u[n]), o[n / 8][n % 8 * 2]);
-        o[n / 8][n % 8 * 2 + 1] = fmaf(f, upper(u[n]), o[n / 8][n % 8 * 2 + 1]);
+        x[n / 8][n % 8 * 2] = fmaf(f, lower(u[n]), x[n / 8][n % 8 * 2] * back);
+        x[n / 8][n % 8 * 2 + 1] = fmaf(f, upper(u[n]), x[n / 8][n % 8 * 2 + 1] * back);
       }
     }
+    L = sum;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) o[d] = x[d];
   }
   const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-  if (!valid) return;
+  if (!valid) continue;
   uint16_t* out = p.out + ((int64_t)(s.first + row / G) * p.q_heads + h * G + row % G) * D + 4 * half;
 #pragma unroll
   for (int d = 0; d < D / 32; ++d)
@@ -722,12 +819,13 @@ __global__ __launch_bounds__(64 * W, 2) void tile_kernel(KvParams p) {
     for (int g = 0; g < 4; ++g)
       *reinterpret_cast<uint2*>(out + 32 * d + 8 * g) =
           make_uint2(pack2<BF16>(o[d][4 * g] * inv, o[d][4 * g + 1] * inv), pack2<BF16>(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv));
+  }
 }
 
-// The grid's second dimension: parts of `chunk` blocks, in a workspace for `units` tiles of `waves` partial results of `floats`
-// each.  Without a workspace one part.
-static unsigned cut(KvParams& p, int64_t units, int64_t blocks, int64_t chunk, int waves, int floats, hipStream_t st) {
-  const size_t bytes = (size_t)units * waves * floats * sizeof(float);
+// The grid's second dimension: parts of `chunk` blocks, in a workspace for `units` tiles of `bytes` and `waves` counters each.
+// Without a workspace one part.
+static unsigned cut(KvParams& p, int64_t units, int64_t blocks, int64_t chunk, int waves, size_t bytes, hipStream_t st) {
+  bytes *= (size_t)units;
   const int64_t counters = units * waves;
   int64_t parts = 1;
   if (layer_knob(5) > 0) chunk = layer_knob(5);
@@ -742,7 +840,7 @@ static unsigned cut(KvParams& p, int64_t units, int64_t blocks, int64_t chunk, i
   return (unsigned)parts;
 }
 
-// Streaming, how long a part is.  Workgroups read at some 40 GB/s each, so as many as there are CUs stream the cache at its rate, and
+// How long a part is.  Workgroups read at some 40 GB/s each, so as many as there are CUs stream the cache at its rate, and
 // more only add partial results; parts of less than four blocks do not pay for their meeting, and parts of at most 128 keep
 // one long sequence among short ones from being the last one left.  One row tile, 64 heads over 8, us:
 //   1 x 131071 tokens (8 units): 32 / 64 / 128 blocks 55 / 48 / 53;    64 x 1000 .. 8000 (512 units): 119 / 114 / 108
@@ -751,22 +849,67 @@ template <int D, bool BF16, bool E4M3, int T>
 static int launch_stream(KvParams& p, int64_t max_tile_rows, int64_t blocks, hipStream_t st) {
   const int64_t tiles = (max_tile_rows + 16 * T - 1) / (16 * T), units = tiles * p.kv_heads * p.batch;
   if (units > MOST_GROUPS) return QG_EUNSUPPORTED;
-  const unsigned parts = cut(p, units, blocks, std::clamp<int64_t>((units * blocks + 255) / 256, 4, 128), 1, PART<D, T>, st);
+  const unsigned parts = cut(p, units, blocks, std::clamp<int64_t>((units * blocks + 255) / 256, 4, 128), 1, PART<D, T> * sizeof(float), st);
   const dim3 grid((unsigned)units, parts), threads(64 * STREAM_WAVES);
   if (tiles > 1) hipLaunchKernelGGL((stream_kernel<D, BF16, E4M3, T, true>), grid, threads, 0, st, p);
   else           hipLaunchKernelGGL((stream_kernel<D, BF16, E4M3, T, false>), grid, threads, 0, st, p);
   return hipGetLastError() == hipSuccess ? QG_OK : QG_EHIP;
 }
 
-// Tiles: parts where there are fewer tiles than the GPU holds at once, of at least eight blocks (800 rows on 4000 tokens: 40 us, uncut 103).
+// A tile's (or share's) part of the workspace: results of W wavefronts, and which place either kind of piece took.
+template <int D, int W>
+constexpr size_t TILE_BYTES = W * (TILE_PART<D> * sizeof(float) + 2 * sizeof(unsigned));
+// Tiles that the GPU holds at once.
+template <int D, int W>
+constexpr int TILES_AT_ONCE = 256 * (D == 64 ? 3 : 8 / W);
+
+// Tiles: parts where there are fewer tiles than the GPU holds at once, of at least eight blocks (800 rows on 4000 tokens: 87 us, uncut 114).
 template <int D, bool BF16, bool E4M3, int W>
 static int launch_tiles(KvParams& p, int64_t max_tile_rows, int64_t blocks, hipStream_t st) {
   const int64_t tiles = (max_tile_rows + 32 * W - 1) / (32 * W), units = tiles * p.kv_heads * p.batch;
   if (units > MOST_GROUPS) return QG_EUNSUPPORTED;
-  constexpr int AT_ONCE = 256 * (D == 64 ? 3 : 8 / W);       // workgroups that the GPU holds
-  const unsigned parts = cut(p, units, blocks, std::max<int64_t>((units * blocks + AT_ONCE - 1) / AT_ONCE, 8), W, TILE_PART<D>, st);
-  hipLaunchKernelGGL((tile_kernel<D, BF16, E4M3, W>), dim3((unsigned)units, parts), dim3(64 * W), 0, st, p);
+  constexpr int AT_ONCE = TILES_AT_ONCE<D, W>;
+  const unsigned parts = cut(p, units, blocks, std::max<int64_t>((units * blocks + AT_ONCE - 1) / AT_ONCE, 8), W, TILE_BYTES<D, W>, st);
+  hipLaunchKernelGGL((tile_kernel<D, BF16, E4M3, W, false>), dim3((unsigned)units, parts), dim3(64 * W), 0, st, p);
   return hipGetLastError() == hipSuccess ? QG_OK : QG_EHIP;
+}
+
+// Tiles in equal shares of at least `least` blocks.  False: not here (no workspace, or more tiles than a workgroup should count).
+template <int D, bool BF16, bool E4M3, int W>
+static bool launch_shares(KvParams& p, int64_t max_tile_rows, int64_t blocks, int least, hipStream_t st, int* rc) {
+  const int64_t tiles = (max_tile_rows + 32 * W - 1) / (32 * W) * p.batch;               // of a head
+  if (tiles > 4096 || tiles * (p.width + 1) >= (1 << 30)) return false;
+  int64_t shares = std::min<int64_t>(TILES_AT_ONCE<D, W>, layer_workspace_bytes() / TILE_BYTES<D, W>) / p.kv_heads;
+  shares = std::min(shares, (tiles * (blocks + 1) + least - 1) / least);
+  if (shares < 2) return false;
+  const int64_t groups = shares * p.kv_heads, counters = groups * W;
+  p.stride = ticket_stride(counters);
+  if (layer_workspace((size_t)groups * TILE_BYTES<D, W>, (size_t)(counters * p.stride), st, &p.partial, &p.tickets) != QG_OK) return false;
+  p.splits = (int)shares;
+  p.least = least;
+  hipLaunchKernelGGL((tile_kernel<D, BF16, E4M3, W, true>), dim3((unsigned)groups), dim3(64 * W), 0, st, p);
+  *rc = hipGetLastError() == hipSuccess ? QG_OK : QG_EHIP;
+  return true;
+}
+
+// Whether shares are the shorter way.  Tiles cost about alike (`blocks`, on average) where there is more history than new rows; then
+// a CU with one tile more than others is what a call waits for, and shares spare that but cost some 10 (64 wide heads) or 14 blocks'
+// time: a cut tile's results go through memory, and its second piece starts anew.  us, whole tiles / shares, rows x sequences on history:
+//   128 wide:  1109 on 5795, 64 heads over 8 343 / 248      up to 614 x 4 on 3500, 40 over 8 149 / 113      up to 300 x 6 on 6000, 64 over 8 266 / 211
+//   64 wide, 40 over 8:  up to 600 x 4 on 3500 99 / 93      2500 on 5000 253 / 229      600 x 4 on 2600 (they fill all places) 100 / 113
+// Without the history it is the other way round, tiles that see little fill the gaps: 4096 on 0, 32 over 8, 128 wide 154 / 212.
+// Where there are few tiles, parts of them cost less than shares and fill the GPU about as well while a share would be short; us, parts / shares:
+//   128 wide:  256 on 30000, 64 over 8 (a share of 117 blocks) 329 / 264      800 on 4000, 32 over 8 (28) 87 / 82      593 on 1285, 16 over 4 (4) 28 / 42
+//   64 wide:   768 on 2212, 64 over 8 (20) 55 / 63      246 on 6023, 32 over 4 (8) 36 / 44
+template <int D, int W>
+static bool shares_pay(const KvParams& p, int64_t max_kv, int64_t G) {
+  if (p.causal && max_kv < 3 * (int64_t)p.max_rows) return false;
+  double tokens = p.causal ? (double)max_kv - 0.5 * p.max_rows : (double)max_kv;
+  if (p.window) tokens = std::min(tokens, (double)p.window + 32.0 * W / G);
+  constexpr int OF_CU = D == 64 ? 3 : 1, FEW = D == 64 ? 512 : 256, COST = D == 64 ? 10 : 14, LONG = D == 64 ? 30 : 20;
+  const double blocks = tokens / KV_BLOCK;
+  const double tiles = ((double)p.rows * G / (32 * W) + 0.5 * p.batch) * p.kv_heads, share = tiles / TILES_AT_ONCE<D, W> * blocks;
+  return share + COST < std::ceil(tiles / 256) / OF_CU * blocks && (tiles > FEW || share >= LONG);
 }
 
 // Which kernel.  The streaming one converts a block for every 32 rows anew and reads it again through the caches, but needs no
@@ -785,12 +928,18 @@ static int launch_attention(KvParams& p, int64_t max_kv, hipStream_t st) {
   const int64_t blocks = std::max<int64_t>((max_kv + KV_BLOCK - 1) / KV_BLOCK, 1), heads = (int64_t)p.kv_heads * p.batch;
   const int forced = layer_knob(4);
   if (forced < 0 || forced > 3 || (forced == 3 && D != 128)) return QG_EINVAL;
+  constexpr int SHARE_WAVES = D == 128 ? 8 : 4;
+  int rc = QG_OK;
+  if (layer_knob(5) < 0)
+    return forced == (D == 128 ? 3 : 2) && launch_shares<D, BF16, E4M3, SHARE_WAVES>(p, rows, blocks, -layer_knob(5), st, &rc) ? rc : QG_EINVAL;
   if (forced == 2) return launch_tiles<D, BF16, E4M3, 4>(p, rows, blocks, st);
   if constexpr (D == 128)
     if (forced == 3) return launch_tiles<D, BF16, E4M3, 8>(p, rows, blocks, st);
   if (rows <= 16) return launch_stream<D, BF16, E4M3, 1>(p, rows, blocks, st);
   const int64_t groups = (rows + 31) / 32 * heads;
   if (forced == 1 || rows <= 192 || (groups <= 512 && groups * blocks <= 20000)) return launch_stream<D, BF16, E4M3, 2>(p, rows, blocks, st);
+  if (shares_pay<D, SHARE_WAVES>(p, max_kv, p.q_heads / p.kv_heads) &&
+      launch_shares<D, BF16, E4M3, SHARE_WAVES>(p, rows, blocks, 8, st, &rc)) return rc;
   if constexpr (D == 128)
     if ((rows + 255) / 256 * heads >= 512) return launch_tiles<D, BF16, E4M3, 8>(p, rows, blocks, st);
   return launch_tiles<D, BF16, E4M3, 4>(p, rows, blocks, st);

@@ -117,7 +117,8 @@ struct KvParams {
   float factor;                        // scale * log2(e)
   int causal;
   int window;                          // 0: none
-  int splits;                          // blocks to a part
+  int splits;                          // blocks to a part; or shares of a head's tiles,
+  int least;                           // and what one of them costs at least
   int stride;                          // of the arrival counters
   float* partial; unsigned* tickets;
 };
