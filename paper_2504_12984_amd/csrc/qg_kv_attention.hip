@@ -564,261 +564,261 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void tile_kernel(KvParams 
     at_end = min(at + each, total);
   }
   while (at < at_end) {
-  int b, tile, skipped = 0, cost = 0;
-  if constexpr (SHARES) {
-    for (;;) {
-      if (c0 >= tiles * B) return;                              // (no: there is a tile at each cost below the total)
-      const int mine = tile_cost<TILE_ROWS>(p, G, c0 + l, tiles);
-      int sum = mine;                                           // of the lanes up to this one
+    int b, tile, skipped = 0, cost = 0;
+    if constexpr (SHARES) {
+      for (;;) {
+        if (c0 >= tiles * B) return;                              // never: below the total there is a tile
+        const int mine = tile_cost<TILE_ROWS>(p, G, c0 + l, tiles);
+        int sum = mine;                                           // of the lanes up to this one
 #pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const int x = __shfl_up(sum, d);
-        if (l >= d) sum += x;
-      }
-      const uint64_t over = __ballot(before + sum > at);
-      if (over) {
-        const int lane = __builtin_ctzll(over);
-        b = (c0 + lane) / tiles; tile = (c0 + lane) % tiles;
-        cost = __builtin_amdgcn_readlane(mine, lane);
-        skipped = at - (before + __builtin_amdgcn_readlane(sum, lane) - cost);
-        break;
-      }
-      before += __builtin_amdgcn_readlane(sum, 63);
-      c0 += 64;
-    }
-  } else {
-    // A workgroup to a tile: tiles that see most first.  The workgroups of a CU come 32 apart: sequences start at another place for
-    // every tile (by the golden section), so that a CU does not get the same one, which may be the longest, again and again.
-    const int nth = group / B;
-    tile = tiles - 1 - nth; b = (int)((group % B + (int64_t)nth * 79 * B / 128) % B);
-  }
-  const Sequence s = sequence(p, b);
-  const int rows = s.rows * G, r0 = tile * TILE_ROWS;
-  if (!SHARES && r0 >= rows) return;
-  const int length = (int)min((int64_t)max(s.length, 0), p.width * KV_BLOCK);
-  const auto place = [&](int row) { return s.before + min(row, rows - 1) / G; };
-  const int from = seen(p, place(r0), length).lo, upto = seen(p, place(r0 + TILE_ROWS - 1), length).hi;
-  const int all = upto > from ? (upto - 1) / KV_BLOCK + 1 - from / KV_BLOCK : 0;
-  // this piece of the tile, the piece'th of `pieces`, and the tile's places in the workspace: place0, place0 + step, ...
-  int first = from / KV_BLOCK, end = first + all, pieces, piece, place0, step;
-  if constexpr (SHARES) {
-    const int start = at - skipped, stop = start + cost, group0 = start / each;
-    pieces = (stop - 1) / each + 1 - group0; piece = group - group0;
-    place0 = group0 * H + h; step = H;
-    end = first + min(min(stop, at_end) - start, all);
-    first += min(skipped, all);
-    at = min(stop, at_end);
-  } else {
-    const int part = max(p.splits, (int)((all + gridDim.y - 1) / gridDim.y));
-    pieces = max((all + part - 1) / part, 1); piece = blockIdx.y;
-    if (piece >= pieces) return;
-    place0 = blockIdx.x * gridDim.y; step = 1;
-    first += piece * part;
-    end = min(first + part, end);
-    at = at_end;
-  }
-  // the wavefront's own rows: seen by some of them, by all of them
-  const int w0 = r0 + wave * 32, row = w0 + i;
-  const Seen seeA = seen(p, place(w0), length), seeZ = seen(p, place(w0 + 31), length);
-  const int w_from = seeA.lo, w_upto = w0 < rows ? seeZ.hi : 0, lo = seeZ.lo, hi = seeA.hi;
-
-  const bool valid = row < rows;
-  Seen see = seen(p, s.before + row / G, length);
-  if (!valid) see.lo = see.hi = 0;
-  half8 q[D / 16];
-  const float cs = load_q_tall<D, BF16>(valid ? p.q + (int64_t)(s.first + row / G) * p.q_stride + (h * G + row % G) * D : nullptr, p.wide, half, q) * p.factor;
-  RowState st = {NONE, 0.0f};
-  float16v o[D / 32];
-#pragma unroll
-  for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
-
-  const int32_t* table = p.table + (int64_t)b * p.width;
-  struct Block : BlockScales { int64_t base; };
-  const auto find = [&](int block) {
-    Block x;
-    const uint32_t id = (uint32_t)table[min(block, end - 1)];
-    x.there = id < (uint64_t)p.num_blocks;
-    x.base = x.there ? (int64_t)id * H + h : 0;
-    x.k = p.k_scale[x.base]; x.v = p.v_scale[x.base];
-    return x;
-  };
-  uint4 raw[HELD];
-  const auto fetch = [&](const Block& x) {
-    const uint4* k = reinterpret_cast<const uint4*>(p.k_cache + x.base * BYTES);
-    const uint4* v = reinterpret_cast<const uint4*>(p.v_cache + x.base * BYTES);
-    if constexpr (EACH) {
-#pragma unroll
-      for (int n = 0; n < EACH; ++n) { raw[n] = k[tid + n * 64 * W]; raw[EACH + n] = v[tid + n * 64 * W]; }
-    } else {
-      raw[0] = tid < PIECES ? k[tid] : v[tid - PIECES];
-    }
-  };
-  // Sixteen dimensions of a token: the two halves of operand (32 tokens, 16 dimensions), lanes of the token.
-  const auto put_k = [&](uint4* at, int piece, uint4 c) {
-    const int t = piece / D, ks = piece / 64 % (D / 64) * 4 + piece % 64 / 16;
-    uint4* to = at + ((t / 2 * (D / 16) + ks) * 64 + t % 2 * 16 + piece % 16);
-    to[0] = __builtin_bit_cast(uint4, numbers<E4M3>(c.x, c.y));
-    to[32] = __builtin_bit_cast(uint4, numbers<E4M3>(c.z, c.w));
-  };
-  // Sixteen tokens of a dimension, four of each of four operands (32 dimensions, 16 tokens).
-  const auto put_v = [&](uint4* at, int piece, uint4 c) {
-    const int f = piece / 64, b4 = piece % 64 / 16;
-    uint2* to = reinterpret_cast<uint2*>(at + (f / 2 * 4 * 64 + b4 % 2 * 32 + f % 2 * 16 + piece % 16)) + b4 / 2;
-    const uint4 lo4 = __builtin_bit_cast(uint4, numbers<E4M3>(c.x, c.y)), hi4 = __builtin_bit_cast(uint4, numbers<E4M3>(c.z, c.w));
-    to[0] = make_uint2(lo4.x, lo4.y); to[128] = make_uint2(lo4.z, lo4.w);
-    to[256] = make_uint2(hi4.x, hi4.y); to[384] = make_uint2(hi4.z, hi4.w);
-  };
-  // bytes of tokens that are not there may be anything, also NaN
-  const auto only_there = [&](uint4 c, int piece, int block, bool there) {
-    if (E4M3 && (!there || block * KV_BLOCK + KV_BLOCK > length)) {
-      const int token0 = block * KV_BLOCK + 4 * (piece % 64 / 16), n = there ? length : 0;
-      c.x &= bytes_below(n - token0); c.y &= bytes_below(n - token0 - 16);
-      c.z &= bytes_below(n - token0 - 32); c.w &= bytes_below(n - token0 - 48);
-    }
-    return c;
-  };
-  const auto stage = [&](int block, bool there) {
-    const int at = block & 1;
-    if constexpr (EACH) {
-#pragma unroll
-      for (int n = 0; n < EACH; ++n) {
-        const int piece = tid + n * 64 * W;
-        put_k(k_sh[at], piece, raw[n]);
-        put_v(v_sh[at], piece, only_there(raw[EACH + n], piece, block, there));
+        for (int d = 1; d < 64; d *= 2) {
+          const int x = __shfl_up(sum, d);
+          if (l >= d) sum += x;
+        }
+        const uint64_t over = __ballot(before + sum > at);
+        if (over) {
+          const int lane = __builtin_ctzll(over);
+          b = (c0 + lane) / tiles; tile = (c0 + lane) % tiles;
+          cost = __builtin_amdgcn_readlane(mine, lane);
+          skipped = at - (before + __builtin_amdgcn_readlane(sum, lane) - cost);
+          break;
+        }
+        before += __builtin_amdgcn_readlane(sum, 63);
+        c0 += 64;
       }
     } else {
-      if (tid < PIECES) put_k(k_sh[at], tid, raw[0]);
-      else              put_v(v_sh[at], tid - PIECES, only_there(raw[0], tid - PIECES, block, there));
+      // A workgroup to a tile: tiles that see most first.  The workgroups of a CU come 32 apart: sequences start at another place for
+      // every tile (by the golden section), so that a CU does not get the same one, which may be the longest, again and again.
+      const int nth = group / B;
+      tile = tiles - 1 - nth; b = (int)((group % B + (int64_t)nth * 79 * B / 128) % B);
     }
-  };
+    const Sequence s = sequence(p, b);
+    const int rows = s.rows * G, r0 = tile * TILE_ROWS;
+    if (!SHARES && r0 >= rows) return;
+    const int length = (int)min((int64_t)max(s.length, 0), p.width * KV_BLOCK);
+    const auto place = [&](int row) { return s.before + min(row, rows - 1) / G; };
+    const int from = seen(p, place(r0), length).lo, upto = seen(p, place(r0 + TILE_ROWS - 1), length).hi;
+    const int all = upto > from ? (upto - 1) / KV_BLOCK + 1 - from / KV_BLOCK : 0;
+    // this piece of the tile, the piece'th of `pieces`, and the tile's places in the workspace: place0, place0 + step, ...
+    int first = from / KV_BLOCK, end = first + all, pieces, piece, place0, step;
+    if constexpr (SHARES) {
+      const int start = at - skipped, stop = start + cost, group0 = start / each;
+      pieces = (stop - 1) / each + 1 - group0; piece = group - group0;
+      place0 = group0 * H + h; step = H;
+      end = first + min(min(stop, at_end) - start, all);
+      first += min(skipped, all);
+      at = min(stop, at_end);
+    } else {
+      const int part = max(p.splits, (int)((all + gridDim.y - 1) / gridDim.y));
+      pieces = max((all + part - 1) / part, 1); piece = blockIdx.y;
+      if (piece >= pieces) return;
+      place0 = blockIdx.x * gridDim.y; step = 1;
+      first += piece * part;
+      end = min(first + part, end);
+      at = at_end;
+    }
+    // the wavefront's own rows: seen by some of them, by all of them
+    const int w0 = r0 + wave * 32, row = w0 + i;
+    const Seen seeA = seen(p, place(w0), length), seeZ = seen(p, place(w0 + 31), length);
+    const int w_from = seeA.lo, w_upto = w0 < rows ? seeZ.hi : 0, lo = seeZ.lo, hi = seeA.hi;
 
-  if (first < end) {
-    Block now = find(first);
-    fetch(now);
-    stage(first, now.there);
-    __syncthreads();
-    for (int block = first; block < end; ++block) {
-      const Block next = find(block + 1);
-      fetch(next);
-      const int t0 = block * KV_BLOCK;
-      if (t0 < w_upto && t0 + KV_BLOCK > w_from) {
-        const uint4* kf = &k_sh[block & 1][l];
-        const uint4* vf = &v_sh[block & 1][l];
-        // operands are read from LDS a group ahead of the matrix instructions that take them: two steps of 16 dimensions,
-        // two tiles of 32 tokens; then a step of 16 tokens, all dimensions
-        half8 a[2][4];
-        const auto read_k = [&](int g) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) a[g & 1][c] = __builtin_bit_cast(half8, kf[(c % 2 * (D / 16) + 2 * g + c / 2) * 64]);
-        };
-        const auto read_v = [&](int g) {
-#pragma unroll
-          for (int d = 0; d < D / 32; ++d) a[g & 1][d] = __builtin_bit_cast(half8, vf[(d * 4 + g) * 64]);
-        };
-        float16v acc[2];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[0][r] = acc[1][r] = 0.0f;
-        read_k(0);
-#pragma unroll
-        for (int g = 0; g < D / 32; ++g) {
-          if (g + 1 < D / 32) read_k(g + 1);
-          else                read_v(0);
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) acc[c % 2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[g & 1][c], q[2 * g + c / 2], acc[c % 2], 0, 0, 0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        half8 P[4];
-        tall_softmax_step(acc, P, o, st, cs, see, now, !now.there || t0 < lo || t0 + KV_BLOCK > hi, t0 + 4 * half);
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          if (g + 1 < 4) read_v(g + 1);
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int d = 0; d < D / 32; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[g & 1][d], P[g], o[d], 0, 0, 0);
-        }
-      }
-      stage(block + 1, next.there);
-      now = next;
-      __syncthreads();
-    }
-  }
-  float L = half_sum(st.l);
-  if (w0 >= rows) continue;
-  if (pieces > 1) {
-    // A wavefront's pieces meet by themselves.  Who is not the last to come leaves its results, as they lie in the lanes; the last
-    // one, which at most waits for others' stores, adds all up in the order of the tokens.
-    constexpr int SIZE = TILE_PART<D>, PAIRS = D / 4;
-    const auto two = [](float x, float y) { return __builtin_bit_cast(uint32_t, x) | (unsigned long long)__builtin_bit_cast(uint32_t, y) << 32; };
-    const auto lower = [](unsigned long long u) { return __builtin_bit_cast(float, (uint32_t)u); };
-    const auto upper = [](unsigned long long u) { return __builtin_bit_cast(float, (uint32_t)(u >> 32)); };
-    const auto at_place = [&](int n) { return (place0 + (int64_t)n * step) * W + wave; };
-    const auto pair_of = [&](int place, int n) { return reinterpret_cast<unsigned long long*>(p.partial + at_place(place) * SIZE) + n * 64 + l; };
-    // which place a piece took: a share ends with one that is a first piece, and begins with one that is not
-    unsigned* const taken = reinterpret_cast<unsigned*>(p.partial + (int64_t)gridDim.x * gridDim.y * W * SIZE);
-    const auto taken_by = [&](int k) { return taken + 2 * at_place(k) + (k == 0); };
-    unsigned* const ticket = p.tickets + ((int64_t)(SHARES ? place0 : (int)blockIdx.x) * W + wave) * p.stride;
-    unsigned came = 0;
-    if (l == 0) came = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    came = __builtin_amdgcn_readfirstlane(came) & 0xffffu;
-    if (came != (unsigned)(pieces - 1)) {
-#pragma unroll
-      for (int n = 0; n < PAIRS; ++n)
-        __hip_atomic_store(pair_of(came, n), two(o[n / 8][n % 8 * 2], o[n / 8][n % 8 * 2 + 1]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __hip_atomic_store(pair_of(came, PAIRS), two(st.m, L), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (l == 0) __hip_atomic_store(taken_by(piece), came, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // they are out before they count
-      if (l == 0) __hip_atomic_fetch_add(ticket, 0x10000u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      continue;
-    }
-    (void)wait_for([&] { return __builtin_amdgcn_readfirstlane(__hip_atomic_load(ticket, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) >> 16; },
-                   (unsigned)(pieces - 1), [] { __builtin_amdgcn_s_sleep(1); });
-    asm volatile("" ::: "memory");                              // nothing is read ahead of the count
-    if (l == 0) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    float16v x[D / 32];
+    const bool valid = row < rows;
+    Seen see = seen(p, s.before + row / G, length);
+    if (!valid) see.lo = see.hi = 0;
+    half8 q[D / 16];
+    const float cs = load_q_tall<D, BF16>(valid ? p.q + (int64_t)(s.first + row / G) * p.q_stride + (h * G + row % G) * D : nullptr, p.wide, half, q) * p.factor;
+    RowState st = {NONE, 0.0f};
+    float16v o[D / 32];
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) x[d][r] = 0.0f;
-    float M = NONE, sum = 0.0f;
-    unsigned took = 0;
-    for (int k = 0; k < pieces; ++k) {
-      if (k % 64 == 0 && k + l < pieces && k + l != piece) took = __hip_atomic_load(taken_by(k + l), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      unsigned long long ml = two(st.m, L), u[PAIRS];
-      if (k == piece) {
+      for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
+
+    const int32_t* table = p.table + (int64_t)b * p.width;
+    struct Block : BlockScales { int64_t base; };
+    const auto find = [&](int block) {
+      Block x;
+      const uint32_t id = (uint32_t)table[min(block, end - 1)];
+      x.there = id < (uint64_t)p.num_blocks;
+      x.base = x.there ? (int64_t)id * H + h : 0;
+      x.k = p.k_scale[x.base]; x.v = p.v_scale[x.base];
+      return x;
+    };
+    uint4 raw[HELD];
+    const auto fetch = [&](const Block& x) {
+      const uint4* k = reinterpret_cast<const uint4*>(p.k_cache + x.base * BYTES);
+      const uint4* v = reinterpret_cast<const uint4*>(p.v_cache + x.base * BYTES);
+      if constexpr (EACH) {
 #pragma unroll
-        for (int n = 0; n < PAIRS; ++n) u[n] = two(o[n / 8][n % 8 * 2], o[n / 8][n % 8 * 2 + 1]);
+        for (int n = 0; n < EACH; ++n) { raw[n] = k[tid + n * 64 * W]; raw[EACH + n] = v[tid + n * 64 * W]; }
       } else {
-        const int place = min(__builtin_amdgcn_readlane(took, k % 64), (unsigned)(pieces - 2));
-        ml = __hip_atomic_load(pair_of(place, PAIRS), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-#pragma unroll
-        for (int n = 0; n < PAIRS; ++n) u[n] = __hip_atomic_load(pair_of(place, n), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        raw[0] = tid < PIECES ? k[tid] : v[tid - PIECES];
       }
-      const float top = fmaxf(M, lower(ml));
-      const float back = top == NONE ? 1.0f : __builtin_amdgcn_exp2f(M - top), f = top == NONE ? 1.0f : __builtin_amdgcn_exp2f(lower(ml) - top);
-      M = top;
-      sum = fmaf(f, upper(ml), sum * back);
+    };
+    // Sixteen dimensions of a token: the two halves of operand (32 tokens, 16 dimensions), lanes of the token.
+    const auto put_k = [&](uint4* at, int piece, uint4 c) {
+      const int t = piece / D, ks = piece / 64 % (D / 64) * 4 + piece % 64 / 16;
+      uint4* to = at + ((t / 2 * (D / 16) + ks) * 64 + t % 2 * 16 + piece % 16);
+      to[0] = __builtin_bit_cast(uint4, numbers<E4M3>(c.x, c.y));
+      to[32] = __builtin_bit_cast(uint4, numbers<E4M3>(c.z, c.w));
+    };
+    // Sixteen tokens of a dimension, four of each of four operands (32 dimensions, 16 tokens).
+    const auto put_v = [&](uint4* at, int piece, uint4 c) {
+      const int f = piece / 64, b4 = piece % 64 / 16;
+      uint2* to = reinterpret_cast<uint2*>(at + (f / 2 * 4 * 64 + b4 % 2 * 32 + f % 2 * 16 + piece % 16)) + b4 / 2;
+      const uint4 lo4 = __builtin_bit_cast(uint4, numbers<E4M3>(c.x, c.y)), hi4 = __builtin_bit_cast(uint4, numbers<E4M3>(c.z, c.w));
+      to[0] = make_uint2(lo4.x, lo4.y); to[128] = make_uint2(lo4.z, lo4.w);
+      to[256] = make_uint2(hi4.x, hi4.y); to[384] = make_uint2(hi4.z, hi4.w);
+    };
+    // bytes of tokens that are not there may be anything, also NaN
+    const auto only_there = [&](uint4 c, int piece, int block, bool there) {
+      if (E4M3 && (!there || block * KV_BLOCK + KV_BLOCK > length)) {
+        const int token0 = block * KV_BLOCK + 4 * (piece % 64 / 16), n = there ? length : 0;
+        c.x &= bytes_below(n - token0); c.y &= bytes_below(n - token0 - 16);
+        c.z &= bytes_below(n - token0 - 32); c.w &= bytes_below(n - token0 - 48);
+      }
+      return c;
+    };
+    const auto stage = [&](int block, bool there) {
+      const int at = block & 1;
+      if constexpr (EACH) {
 #pragma unroll
-      for (int n = 0; n < PAIRS; ++n) {
-        x[n / 8][n % 8 * 2] = fmaf(f, lower(u[n]), x[n / 8][n % 8 * 2] * back);
-        x[n / 8][n % 8 * 2 + 1] = fmaf(f, upper(u[n]), x[n / 8][n % 8 * 2 + 1] * back);
+        for (int n = 0; n < EACH; ++n) {
+          const int piece = tid + n * 64 * W;
+          put_k(k_sh[at], piece, raw[n]);
+          put_v(v_sh[at], piece, only_there(raw[EACH + n], piece, block, there));
+        }
+      } else {
+        if (tid < PIECES) put_k(k_sh[at], tid, raw[0]);
+        else              put_v(v_sh[at], tid - PIECES, only_there(raw[0], tid - PIECES, block, there));
+      }
+    };
+
+    if (first < end) {
+      Block now = find(first);
+      fetch(now);
+      stage(first, now.there);
+      __syncthreads();
+      for (int block = first; block < end; ++block) {
+        const Block next = find(block + 1);
+        fetch(next);
+        const int t0 = block * KV_BLOCK;
+        if (t0 < w_upto && t0 + KV_BLOCK > w_from) {
+          const uint4* kf = &k_sh[block & 1][l];
+          const uint4* vf = &v_sh[block & 1][l];
+          // operands are read from LDS a group ahead of the matrix instructions that take them: two steps of 16 dimensions,
+          // two tiles of 32 tokens; then a step of 16 tokens, all dimensions
+          half8 a[2][4];
+          const auto read_k = [&](int g) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) a[g & 1][c] = __builtin_bit_cast(half8, kf[(c % 2 * (D / 16) + 2 * g + c / 2) * 64]);
+          };
+          const auto read_v = [&](int g) {
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) a[g & 1][d] = __builtin_bit_cast(half8, vf[(d * 4 + g) * 64]);
+          };
+          float16v acc[2];
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[0][r] = acc[1][r] = 0.0f;
+          read_k(0);
+#pragma unroll
+          for (int g = 0; g < D / 32; ++g) {
+            if (g + 1 < D / 32) read_k(g + 1);
+            else                read_v(0);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) acc[c % 2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[g & 1][c], q[2 * g + c / 2], acc[c % 2], 0, 0, 0);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          half8 P[4];
+          tall_softmax_step(acc, P, o, st, cs, see, now, !now.there || t0 < lo || t0 + KV_BLOCK > hi, t0 + 4 * half);
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            if (g + 1 < 4) read_v(g + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[g & 1][d], P[g], o[d], 0, 0, 0);
+          }
+        }
+        stage(block + 1, next.there);
+        now = next;
+        __syncthreads();
       }
     }
-    L = sum;
+    float L = half_sum(st.l);
+    if (w0 >= rows) continue;
+    if (pieces > 1) {
+      // A wavefront's pieces meet by themselves.  Who is not the last to come leaves its results, as they lie in the lanes; the last
+      // one, which at most waits for others' stores, adds all up in the order of the tokens.
+      constexpr int SIZE = TILE_PART<D>, PAIRS = D / 4;
+      const auto two = [](float x, float y) { return __builtin_bit_cast(uint32_t, x) | (unsigned long long)__builtin_bit_cast(uint32_t, y) << 32; };
+      const auto lower = [](unsigned long long u) { return __builtin_bit_cast(float, (uint32_t)u); };
+      const auto upper = [](unsigned long long u) { return __builtin_bit_cast(float, (uint32_t)(u >> 32)); };
+      const auto at_place = [&](int n) { return (place0 + (int64_t)n * step) * W + wave; };
+      const auto pair_of = [&](int place, int n) { return reinterpret_cast<unsigned long long*>(p.partial + at_place(place) * SIZE) + n * 64 + l; };
+      // which place a piece took: a share ends with one that is a first piece, and begins with one that is not
+      unsigned* const taken = reinterpret_cast<unsigned*>(p.partial + (int64_t)gridDim.x * gridDim.y * W * SIZE);
+      const auto taken_by = [&](int k) { return taken + 2 * at_place(k) + (k == 0); };
+      unsigned* const ticket = p.tickets + ((int64_t)(SHARES ? place0 : (int)blockIdx.x) * W + wave) * p.stride;
+      unsigned came = 0;
+      if (l == 0) came = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      came = __builtin_amdgcn_readfirstlane(came) & 0xffffu;
+      if (came != (unsigned)(pieces - 1)) {
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d) o[d] = x[d];
-  }
-  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-  if (!valid) continue;
-  uint16_t* out = p.out + ((int64_t)(s.first + row / G) * p.q_heads + h * G + row % G) * D + 4 * half;
+        for (int n = 0; n < PAIRS; ++n)
+          __hip_atomic_store(pair_of(came, n), two(o[n / 8][n % 8 * 2], o[n / 8][n % 8 * 2 + 1]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(pair_of(came, PAIRS), two(st.m, L), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (l == 0) __hip_atomic_store(taken_by(piece), came, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // they are out before they count
+        if (l == 0) __hip_atomic_fetch_add(ticket, 0x10000u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        continue;
+      }
+      (void)wait_for([&] { return __builtin_amdgcn_readfirstlane(__hip_atomic_load(ticket, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) >> 16; },
+                     (unsigned)(pieces - 1), [] { __builtin_amdgcn_s_sleep(1); });
+      asm volatile("" ::: "memory");                              // nothing is read ahead of the count
+      if (l == 0) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      float16v x[D / 32];
 #pragma unroll
-  for (int d = 0; d < D / 32; ++d)
+      for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *reinterpret_cast<uint2*>(out + 32 * d + 8 * g) =
-          make_uint2(pack2<BF16>(o[d][4 * g] * inv, o[d][4 * g + 1] * inv), pack2<BF16>(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv));
+        for (int r = 0; r < 16; ++r) x[d][r] = 0.0f;
+      float M = NONE, sum = 0.0f;
+      unsigned took = 0;
+      for (int k = 0; k < pieces; ++k) {
+        if (k % 64 == 0 && k + l < pieces && k + l != piece) took = __hip_atomic_load(taken_by(k + l), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        unsigned long long ml = two(st.m, L), u[PAIRS];
+        if (k == piece) {
+#pragma unroll
+          for (int n = 0; n < PAIRS; ++n) u[n] = two(o[n / 8][n % 8 * 2], o[n / 8][n % 8 * 2 + 1]);
+        } else {
+          const int place = min(__builtin_amdgcn_readlane(took, k % 64), (unsigned)(pieces - 2));
+          ml = __hip_atomic_load(pair_of(place, PAIRS), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+          for (int n = 0; n < PAIRS; ++n) u[n] = __hip_atomic_load(pair_of(place, n), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        const float top = fmaxf(M, lower(ml));
+        const float back = top == NONE ? 1.0f : __builtin_amdgcn_exp2f(M - top), f = top == NONE ? 1.0f : __builtin_amdgcn_exp2f(lower(ml) - top);
+        M = top;
+        sum = fmaf(f, upper(ml), sum * back);
+#pragma unroll
+        for (int n = 0; n < PAIRS; ++n) {
+          x[n / 8][n % 8 * 2] = fmaf(f, lower(u[n]), x[n / 8][n % 8 * 2] * back);
+          x[n / 8][n % 8 * 2 + 1] = fmaf(f, upper(u[n]), x[n / 8][n % 8 * 2 + 1] * back);
+        }
+      }
+      L = sum;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) o[d] = x[d];
+    }
+    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+    if (!valid) continue;
+    uint16_t* out = p.out + ((int64_t)(s.first + row / G) * p.q_heads + h * G + row % G) * D + 4 * half;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<uint2*>(out + 32 * d + 8 * g) =
+            make_uint2(pack2<BF16>(o[d][4 * g] * inv, o[d][4 * g + 1] * inv), pack2<BF16>(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv));
   }
 }
 
