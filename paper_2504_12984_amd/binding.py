@@ -409,7 +409,8 @@ def qg_rmsnorm_a8(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: t
         r_ptr, r_stride = _rows(residual, "residual", shape, dtype)
         if sum_out is None:
             sum_out = torch.empty_like(x, memory_format=torch.contiguous_format)
-    if sum_out is not None:
+            s_ptr, s_stride = sum_out.data_ptr(), N
+    if s_ptr is None and sum_out is not None:
         s_ptr, s_stride = _rows(sum_out, "sum_out", shape, dtype)
     A8 = torch.empty_like(x, dtype=torch.int8, memory_format=torch.contiguous_format)
     a_scale = x.new_empty(M, dtype=torch.float32)
@@ -431,7 +432,7 @@ def qg_silu_a8(gate: torch.Tensor, up: torch.Tensor | None = None):
         u_ptr, u_stride = g_ptr + 2 * N, g_stride
     else:
         u_ptr, u_stride = _rows(up, "up", shape, dtype)
-    A8 = gate.new_empty((M, N), dtype=torch.int8)
+    A8 = gate.new_empty(M, N, dtype=torch.int8)
     a_scale = gate.new_empty(M, dtype=torch.float32)
     _check("qg_silu_a8", _lib.qg_silu_a8(g_ptr, u_ptr, _DT[dtype], M, N, g_stride, u_stride, A8.data_ptr(), a_scale.data_ptr(),
                                          _stream()))
@@ -497,7 +498,7 @@ def qg_kv_append(k: torch.Tensor, v: torch.Tensor, cache: KvCache, row_start: to
         shape = torch.Size((rows, q_heads, D))
         q_ptr, q_stride = _rows(q, "q", shape, dtype)
         if q_out is None:
-            q_out = k.new_empty(shape)
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif q_out.shape != shape or q_out.dtype is not dtype:
             raise ValueError("q_out must be q's shape and type")
     positions, rot = 0, 0
@@ -524,7 +525,7 @@ def qg_kv_attention(q: torch.Tensor, cache: KvCache, row_start: torch.Tensor, kv
         raise ValueError("q must be [rows, heads, head_dim] with the cache's head_dim")
     q_ptr, q_stride = _rows(q, "q", shape, dtype)
     if out is None:
-        out = q.new_empty(shape)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     elif out.shape != shape or out.dtype is not dtype:
         raise ValueError("out must be q's shape and type")
     s_ptr, l_ptr, t_ptr, width, batch = _sequences(row_start, kv_len, block_table)
